@@ -399,9 +399,154 @@ nmt_status nmt_score_ensemble(int32_t K, nmt_model* const* models, const nmt_sou
                               const float* h_weights, float* d_score, void* d_workspace, size_t ws_bytes,
                               void* stream);
 
+/* ---------------------------------------------------------- drafted words
+ *
+ * A cheap proposer (a small model, a model whose output layer is held in 4
+ * bits, a phrase table) drafts several words after a hypothesis; the full
+ * model then keeps the drafts that its own distribution keeps and adds one
+ * word, so that what is emitted is distributed as the full model's own words.
+ * One round over S sequences:
+ *   nmt_step_readouts  -- the positions' states and readouts, one call per
+ *                         position (each needs the state of the one before);
+ *   nmt_logits         -- all positions' next-word logits in one call, which
+ *                         reads the output weights once;
+ *   nmt_w4_product     -- the proposer's logits from its readouts;
+ *   nmt_verify_drafts  -- how many drafts of each sequence are kept, and the
+ *                         word after them. */
+
+/* nmt_score_batch without the vocabulary: B rows' new states and readouts
+ * (the model's t, the output layer's input).
+ *   d_state_pool [pool_rows x H], d_state_row [B]  row b's input state is
+ *                     d_state_pool[d_state_row[b]]; d_state_row NULL: row b of
+ *                     the pool (pool_rows >= B)
+ *   d_y_prev, d_sent_id [B]  as for nmt_score_batch
+ *   d_s_new [B x H]   out: new states.  With d_state_row it must not overlap
+ *                     the pool; without, it may be the pool itself.
+ *   d_t [B x E]       out: readouts (fp32; bf16 models: at bf16 values)
+ * Workspace as for nmt_score_batch with the same B.  A row with an id out of
+ * range gets NaN readouts and sets the device error flag.  B = 0 is a no-op.
+ * Errors: NMT_EINVAL, NMT_EWORKSPACE, NMT_EDEVICE. */
+nmt_status nmt_step_readouts(nmt_model* m, const nmt_source* src, int32_t B, const float* d_state_pool,
+                             int32_t pool_rows, const int32_t* d_state_row, const int32_t* d_y_prev,
+                             const int32_t* d_sent_id, float* d_s_new, float* d_t, void* d_workspace,
+                             size_t ws_bytes, void* stream);
+
+/* The logits of every next word of M readouts: z = t out_W + out_b.
+ *   d_t [M x E]       readouts (any fp32 values; a bf16 model rounds them to
+ *                     bf16, nearest even).  A row that holds an infinity or a
+ *                     NaN gets logits that are not finite.
+ *   d_logits          out: row i at d_logits + i * ld_logits, V fp32 values
+ *                     (ld_logits >= V; what lies between rows is not written)
+ *   d_logZ [M]        out, nullable: log sum_v exp(z_v)
+ * Workspace as for nmt_score_batch with B = M.  Rows are independent.  M = 0
+ * is a no-op.  Errors: NMT_EINVAL, NMT_EWORKSPACE, NMT_EDEVICE. */
+nmt_status nmt_logits(nmt_model* m, int32_t M, const float* d_t, float* d_logits, int64_t ld_logits, float* d_logZ,
+                      void* d_workspace, size_t ws_bytes, void* stream);
+
+/* A matrix of 4-bit weights: K x N codes c in [0, 15], and for every group of
+ * `group` consecutive rows of a column a scale s and a zero point z, standing
+ * for the weight s (c - z); the last group is shorter where K is no multiple
+ * of it.  Read-only once made; products on any stream may share it. */
+typedef struct nmt_w4 nmt_w4;
+
+typedef struct {
+  int32_t K, N;   /* rows (inputs) and columns (outputs), >= 1 */
+  int32_t group;  /* rows per scale: a positive multiple of 32 */
+  int32_t stype;  /* nmt_dtype of the scales on the device (NMT_BF16: rounded, nearest even) */
+} nmt_w4_dims;
+
+/* Copy a 4-bit matrix to the current HIP device, laid out for the kernel.
+ *   h_codes  [K x ceil(N/2)] bytes, row-major: byte i of a row holds the codes
+ *            of columns 2i (low half) and 2i + 1 (high half)
+ *   h_scales [ceil(K/group) x N] fp32, finite (with NMT_BF16 also once rounded)
+ *   h_zeros  [ceil(K/group) x N] bytes in [0, 15]; NULL: 8 everywhere
+ *   h_bias   [N] fp32, added to every product; NULL: none
+ * The caller keeps the host arrays.  Synchronous.  Errors: NMT_EINVAL, NMT_ERANGE
+ * (a zero point above 15), NMT_ENOMEM, NMT_EDEVICE. */
+nmt_status nmt_w4_create(const nmt_w4_dims* dims, const uint8_t* h_codes, const float* h_scales,
+                         const uint8_t* h_zeros, const float* h_bias, nmt_w4** out);
+
+/* A 4-bit copy of a model's output layer (K = E, N = V, with its bias), for
+ * drafting with that model: s = the group's largest |w| / 7, rounded to the
+ * scales' type, c = 8 + w / s rounded to the nearest (ties to even) within
+ * [1, 15], z = 8; a group whose scale comes out 0 holds zeros.  Runs on
+ * `stream` and waits for it.  Independent of the model afterwards.
+ * Errors: NMT_EINVAL (also for a layer with a weight that is not finite),
+ * NMT_ENOMEM, NMT_EDEVICE. */
+nmt_status nmt_w4_from_output(const nmt_model* m, int32_t group, int32_t stype, void* stream, nmt_w4** out);
+
+/* The matrix's sizes, and whether it has zero points of its own and a bias.
+ * Any output may be NULL. */
+nmt_status nmt_w4_info(const nmt_w4* w, nmt_w4_dims* dims, int32_t* has_zeros, int32_t* has_bias);
+
+/* y = x W (+ bias) for M rows, W a 4-bit matrix.
+ *   d_x   row i at x + i * ld_x elements of x_type, K values (ld_x >= K)
+ *   d_y   out: row i at y + i * ld_y elements of y_type, N values (ld_y >= N;
+ *         what lies between rows is not written); must not overlap x
+ * Products and sums are fp32 (fp32 inputs enter with 22 significant bits or
+ * more, relative to the largest of each 128 inputs); bf16 outputs are rounded
+ * once, nearest even.  Infinities and NaN in x reach the row's outputs as in
+ * fp32 products.  Pointers need their element's alignment only (16-byte
+ * aligned rows are read and written faster).  Rows are independent: a row's
+ * outputs do not depend on the others' values.  M = 0 is a no-op; the call
+ * allocates nothing and needs no workspace.  Errors: NMT_EINVAL, NMT_EDEVICE. */
+nmt_status nmt_w4_product(const nmt_w4* w, int32_t M, const void* d_x, int32_t x_type, int64_t ld_x, void* d_y,
+                          int32_t y_type, int64_t ld_y, void* stream);
+
+/* Free a 4-bit matrix (waits for the device first).  NULL is a no-op. */
+void nmt_w4_destroy(nmt_w4* w);
+
+/* Bytes of device workspace that serve nmt_verify_drafts for at most S
+ * sequences with at most n_draft drafts in all under model m.  0 for invalid
+ * arguments. */
+size_t nmt_verify_workspace_bytes(const nmt_model* m, int32_t S, int32_t n_draft);
+
+/* Which drafted words the model's distributions keep, and the word after them.
+ * Sequence s has the drafts d_draft[d_draft_off[s] .. d_draft_off[s+1]), n_s of
+ * them (possibly none), and n_s + 1 rows of target logits: row
+ * d_draft_off[s] + s + j is the model's distribution p_j (softmax of the row)
+ * of the word at position j, after drafts 0 .. j-1.  d_u holds one random
+ * number for each of these rows.  Draft j is kept if every one before it is
+ * and u_j q_j(d_j) < p_j(d_j), where q_j is the distribution that it was drawn
+ * from: proposal row d_draft_off[s] + j, or, without proposals, certainty
+ * (q_j(d_j) = 1).  With a kept drafts the word after them is drawn from
+ *   a < n_s:  max(p_a - q_a, 0), normalised (p_a without d_a, where there are
+ *             no proposals; p_a itself where nothing is left, which takes a
+ *             draft of probability 0 under both);
+ *   a = n_s:  p_a
+ * as the lowest word whose running sum exceeds u_{n_s} times the whole sum
+ * (the sequence's last random number).  With no drafts at all the call samples
+ * one word from each row.
+ *   d_draft_off [S+1]  CSR offsets, non-decreasing, in [0, n_draft]
+ *   d_draft [n_draft]  drafted words, in [0, V)
+ *   d_target           n_draft + S rows of V logits, row stride ld_target >= V
+ *                      elements of target_type; -infinity: probability 0
+ *   d_proposal         n_draft rows of V logits likewise, or NULL
+ *   d_u [n_draft + S]  random numbers in [0, 1)
+ *   d_accepted [S]     out: a
+ *   d_next [S]         out: the word after the kept drafts
+ *   d_draft_logp [n_draft]  out, nullable: log p_j(d_j) of every draft, kept
+ *                      or not (NaN where the draft or the row is no good)
+ *   d_next_logp [S]    out, nullable: log p_a of d_next
+ * Sums and comparisons are in 64 bits.  Logits need their element's alignment
+ * only (16-byte aligned rows are read faster).  A sequence with malformed
+ * offsets, or that reaches a draft out of range or a row that is no
+ * distribution (NaN, +infinity or nothing above -infinity), keeps the drafts
+ * before it, gets d_next = -1 and log p = NaN, and sets the model's device
+ * error flag.  Sequences are independent.  S = 0 is a no-op.  The call
+ * allocates nothing; calls on different streams must use different workspaces.
+ * d_workspace: nmt_verify_workspace_bytes bytes, 256-byte aligned.
+ * Errors: NMT_EINVAL, NMT_EWORKSPACE, NMT_EDEVICE. */
+nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int32_t* d_draft_off,
+                             const int32_t* d_draft, const void* d_target, int32_t target_type, int64_t ld_target,
+                             const void* d_proposal, int32_t proposal_type, int64_t ld_proposal, const float* d_u,
+                             int32_t* d_accepted, int32_t* d_next, float* d_draft_logp, float* d_next_logp,
+                             void* d_workspace, size_t ws_bytes, void* stream);
+
 /* Wait for `stream`, then report and clear the model's device error flag:
- * NMT_ERANGE if any call since the last check met an out-of-range id,
- * NMT_EDEVICE on a HIP error, else NMT_OK. */
+ * NMT_ERANGE if any call since the last check met an out-of-range id (or
+ * nmt_verify_drafts a row that is no distribution), NMT_EDEVICE on a HIP
+ * error, else NMT_OK. */
 nmt_status nmt_stream_status(nmt_model* m, void* stream);
 
 /* Message for the last failed call on this thread ("" if none). */

@@ -39,16 +39,23 @@ EXPORTS = ("nmt_model_create", "nmt_model_destroy", "nmt_encode", "nmt_source_fr
            "nmt_forest_destroy", "nmt_model_average", "nmt_ensemble_workspace_bytes", "nmt_score_ensemble",
            "nmt_rescorer_create", "nmt_rescore_stack", "nmt_rescorer_info", "nmt_rescorer_destroy",
            "nmt_debug_alloc_hook", "nmt_debug_gemm_form", "nmt_debug_gemm_streamed", "nmt_debug_precompute",
-           "nmt_debug_small_step", "nmt_debug_encode_form")
+           "nmt_debug_small_step", "nmt_debug_encode_form",
+           "nmt_step_readouts", "nmt_logits", "nmt_w4_create", "nmt_w4_from_output", "nmt_w4_info",
+           "nmt_w4_product", "nmt_w4_destroy", "nmt_verify_workspace_bytes", "nmt_verify_drafts")
 
 PHASES = ("gru1", "query", "attention", "gru2", "readout", "vocab", "combine")
 
 _VP = ctypes.c_void_p
 _I32 = ctypes.c_int32
+_I64 = ctypes.c_int64
 
 
 class Dims(ctypes.Structure):
     _fields_ = [("V_src", _I32), ("V", _I32), ("E", _I32), ("H", _I32), ("A", _I32), ("wtype", _I32)]
+
+
+class W4Dims(ctypes.Structure):
+    _fields_ = [("K", _I32), ("N", _I32), ("group", _I32), ("stype", _I32)]
 
 
 class Weights(ctypes.Structure):
@@ -116,6 +123,19 @@ def load_library(path: str = LIB_PATH):
     lib.nmt_rescorer_info.argtypes = [_VP, _I32, P(_VP), IP, IP, IP, IP, IP]
     lib.nmt_rescorer_destroy.argtypes = [_VP]
     lib.nmt_rescorer_destroy.restype = None
+    SZ = ctypes.c_size_t
+    lib.nmt_step_readouts.argtypes = [_VP, _VP, _I32, _VP, _I32, _VP, _VP, _VP, _VP, _VP, _VP, SZ, _VP]
+    lib.nmt_logits.argtypes = [_VP, _I32, _VP, _VP, _I64, _VP, _VP, SZ, _VP]
+    lib.nmt_w4_create.argtypes = [P(W4Dims), _VP, _VP, _VP, _VP, P(_VP)]
+    lib.nmt_w4_from_output.argtypes = [_VP, _I32, _I32, _VP, P(_VP)]
+    lib.nmt_w4_info.argtypes = [_VP, P(W4Dims), IP, IP]
+    lib.nmt_w4_product.argtypes = [_VP, _I32, _VP, _I32, _I64, _VP, _I32, _I64, _VP]
+    lib.nmt_w4_destroy.argtypes = [_VP]
+    lib.nmt_w4_destroy.restype = None
+    lib.nmt_verify_workspace_bytes.argtypes = [_VP, _I32, _I32]
+    lib.nmt_verify_workspace_bytes.restype = SZ
+    lib.nmt_verify_drafts.argtypes = [_VP, _I32, _I32, _VP, _VP, _VP, _I32, _I64, _VP, _I32, _I64, _VP, _VP, _VP, _VP,
+                                      _VP, _VP, SZ, _VP]
     lib.nmt_debug_alloc_hook.argtypes = [_I32]
     lib.nmt_debug_alloc_hook.restype = ctypes.c_int64
     lib.nmt_debug_gemm_form.argtypes = [_I32]
@@ -134,7 +154,9 @@ def load_library(path: str = LIB_PATH):
               "nmt_score_batch", "nmt_score_batch_debug", "nmt_score_batch_noalloc", "nmt_stream_status", "nmt_profile_begin",
               "nmt_profile_end", "nmt_score_forest_step", "nmt_forest_build", "nmt_forest_shape",
               "nmt_forest_level", "nmt_forest_pair_paths", "nmt_score_forest", "nmt_model_average",
-              "nmt_score_ensemble", "nmt_rescorer_create", "nmt_rescore_stack", "nmt_rescorer_info"):
+              "nmt_score_ensemble", "nmt_rescorer_create", "nmt_rescore_stack", "nmt_rescorer_info",
+              "nmt_step_readouts", "nmt_logits", "nmt_w4_create", "nmt_w4_from_output", "nmt_w4_info",
+              "nmt_w4_product", "nmt_verify_drafts"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -200,6 +222,29 @@ def _ptr(t) -> Optional[int]:
     if not t.is_contiguous():
         raise ValueError("expected a contiguous tensor")
     return t.data_ptr()
+
+
+def _rows(t, cols: int, rows: int):
+    """(address, element type, row stride) of a device matrix of fp32 or bf16
+    rows; the elements of a row must be consecutive."""
+    import torch
+    types = {torch.float32: NMT_F32, torch.bfloat16: NMT_BF16}
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    if t.dtype not in types:
+        raise ValueError(f"expected fp32 or bf16 elements, got {t.dtype}")
+    if t.dim() != 2 or tuple(t.shape) != (rows, cols):
+        raise ValueError(f"expected a [{rows}, {cols}] tensor, got {tuple(t.shape)}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("expected rows of consecutive elements")
+    return t.data_ptr(), types[t.dtype], t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _checked(t, dtype, n: int, what: str):
+    """Device address of a contiguous tensor with n elements of dtype (None stays NULL)."""
+    if t is not None and (t.dtype != dtype or t.numel() != n):
+        raise ValueError(f"{what}: expected {n} elements of {dtype}, got {t.numel()} of {t.dtype}")
+    return _ptr(t)
 
 
 def _stream(stream) -> Optional[int]:
@@ -430,6 +475,119 @@ def nmt_score_forest_step(model: Model, src: Source, state_pool, state_row, y_pr
                                      _ptr(state_row), _ptr(y_prev), _ptr(sent_id), _ptr(req_off), _ptr(req),
                                      int(req.shape[0]), _ptr(logp), _ptr(s_new), _ptr(logZ), _ptr(workspace),
                                      workspace.numel(), _stream(stream)))
+
+
+class W4:
+    """A 4-bit matrix (nmt_w4): codes [K, ceil(N/2)] uint8, two columns a byte (the lower column in the
+    low half), scales [ceil(K/group), N] fp32, zeros likewise uint8 (None: 8), bias [N] fp32 (None: none);
+    stype "f32" or "bf16": the scales' type on the device."""
+
+    def __init__(self, codes, scales, K: int, N: int, group: int, zeros=None, bias=None, stype: str = "f32"):
+        G = -(-K // group) if group > 0 else 0
+        arr = lambda a, t, shape, what: None if a is None else self._host(a, t, shape, what)
+        keep = [arr(codes, np.uint8, (K, (N + 1) // 2), "codes"), arr(scales, np.float32, (G, N), "scales"),
+                arr(zeros, np.uint8, (G, N), "zeros"), arr(bias, np.float32, (N,), "bias")]
+        h = _VP()
+        dims = W4Dims(K, N, group, _stype(stype))
+        _check(load_library().nmt_w4_create(ctypes.byref(dims), *[None if a is None else a.ctypes.data for a in keep],
+                                            ctypes.byref(h)))
+        self.handle, self.K, self.N, self.group = h, K, N, group
+
+    @staticmethod
+    def _host(a, dtype, shape, what):
+        a = np.ascontiguousarray(a, dtype=dtype)
+        if a.shape != shape:
+            raise ValueError(f"{what}: expected shape {shape}, got {a.shape}")
+        return a
+
+    @classmethod
+    def from_output(cls, model: Model, group: int = 64, stype: str = "f32", stream=None) -> "W4":
+        """A 4-bit copy of the model's output layer (K = E, N = V)."""
+        h = _VP()
+        _check(load_library().nmt_w4_from_output(model.handle, group, _stype(stype), _stream(stream), ctypes.byref(h)))
+        w = cls.__new__(cls)
+        w.handle, w.K, w.N, w.group = h, model.E, model.V, group
+        return w
+
+    def info(self) -> dict:
+        d, z, b = W4Dims(), _I32(), _I32()
+        _check(load_library().nmt_w4_info(self.handle, ctypes.byref(d), ctypes.byref(z), ctypes.byref(b)))
+        return {"K": d.K, "N": d.N, "group": d.group, "stype": "bf16" if d.stype == NMT_BF16 else "f32",
+                "zeros": bool(z.value), "bias": bool(b.value)}
+
+    def close(self):
+        if getattr(self, "handle", None):
+            load_library().nmt_w4_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _stype(name: str) -> int:
+    if name not in ("f32", "bf16"):
+        raise ValueError(f"unknown type {name!r}")
+    return NMT_BF16 if name == "bf16" else NMT_F32
+
+
+def nmt_w4_product(w: W4, x, y, stream=None):
+    """y = x W (+ bias): x [M, K] and y [M, N], fp32 or bf16, rows at any stride."""
+    M = int(x.shape[0])
+    xp, xt, xl = _rows(x, w.K, M)
+    yp, yt, yl = _rows(y, w.N, M)
+    _check(load_library().nmt_w4_product(w.handle, M, xp, xt, xl, yp, yt, yl, _stream(stream)))
+
+
+def nmt_step_readouts(model: Model, src: Source, state_pool, y_prev, sent_id, s_new, t, state_row=None,
+                      workspace=None, stream=None):
+    """One step without the vocabulary: new states and readouts t [B, E] (see nmt.h)."""
+    import torch
+    B = int(y_prev.shape[0])
+    if workspace is None:
+        workspace = torch.empty(max(nmt_score_workspace_bytes(model, B), 256), dtype=torch.uint8, device="cuda")
+    _check(load_library().nmt_step_readouts(
+        model.handle, src.handle, B, _ptr(state_pool), int(state_pool.shape[0]),
+        _checked(state_row, torch.int32, B, "state_row"), _checked(y_prev, torch.int32, B, "y_prev"),
+        _checked(sent_id, torch.int32, B, "sent_id"), _checked(s_new, torch.float32, B * model.H, "s_new"),
+        _checked(t, torch.float32, B * model.E, "t"), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def nmt_logits(model: Model, t, logits, logZ=None, workspace=None, stream=None):
+    """The logits [M, V] of every next word of readouts t [M, E] (rows of logits at any stride)."""
+    import torch
+    M = int(t.shape[0])
+    if workspace is None:
+        workspace = torch.empty(max(nmt_score_workspace_bytes(model, M), 256), dtype=torch.uint8, device="cuda")
+    zp, zt, zl = _rows(logits, model.V, M)
+    if zt != NMT_F32:
+        raise ValueError("logits must be fp32")
+    _check(load_library().nmt_logits(model.handle, M, _checked(t, torch.float32, M * model.E, "t"), zp, zl,
+                                     _checked(logZ, torch.float32, M, "logZ"), _ptr(workspace), workspace.numel(),
+                                     _stream(stream)))
+
+
+def nmt_verify_workspace_bytes(model: Model, S: int, n_draft: int) -> int:
+    return int(load_library().nmt_verify_workspace_bytes(model.handle, S, n_draft))
+
+
+def nmt_verify_drafts(model: Model, draft_off, draft, target, proposal, u, accepted, next_word, draft_logp=None,
+                      next_logp=None, workspace=None, stream=None):
+    """How many drafted words of each sequence the target's distributions keep, and the word after them (see
+    nmt.h): draft_off [S+1], draft [n], target [n + S, V] logits, proposal [n, V] logits or None, u [n + S]."""
+    import torch
+    S, n, i32, f32 = int(draft_off.shape[0]) - 1, int(draft.shape[0]), torch.int32, torch.float32
+    if workspace is None:
+        workspace = torch.empty(max(nmt_verify_workspace_bytes(model, S, n), 256), dtype=torch.uint8, device="cuda")
+    tp, tt, tl = _rows(target, model.V, n + S)
+    pp, pt, pl = (None, NMT_F32, 0) if proposal is None or n == 0 else _rows(proposal, model.V, n)
+    _check(load_library().nmt_verify_drafts(
+        model.handle, S, n, _checked(draft_off, i32, S + 1, "draft_off"), _checked(draft, i32, n, "draft"), tp, tt, tl,
+        pp, pt, pl, _checked(u, f32, n + S, "u"), _checked(accepted, i32, S, "accepted"),
+        _checked(next_word, i32, S, "next_word"), _checked(draft_logp, f32, n, "draft_logp"),
+        _checked(next_logp, f32, S, "next_logp"), _ptr(workspace), workspace.numel(), _stream(stream)))
 
 
 def _i32p(a):

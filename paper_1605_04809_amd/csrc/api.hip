@@ -19,6 +19,7 @@
 #include "../../include/nmt.h"
 #include "../../include/nmt_debug.h"
 #include "../../include/nmt_profile.h"
+#include "draft.hpp"
 #include "internal.hpp"
 
 using namespace nmt;
@@ -495,6 +496,7 @@ hipError_t split_weights(nmt_model* m, hipStream_t st) {
   // biases that are finite must stay so in the accumulators' units
   const float most_bias = __builtin_bit_cast(float, range[kBias].most);
   if (!fits || !std::isfinite(std::ldexp(most_bias, bias_scale))) m->out.sp = SplitW{};
+  for (int& r = m->out.sp.bias_room; r < kSplitBiasRoom && std::isfinite(std::ldexp(most_bias, bias_scale + r + 1));) ++r;
   fits = wide;
   for (int i = 0; i < kItems && fits; ++i) fits = plan(all[i], range[i], false);
   for (int i = 0; i < 2 && fits; ++i) {
@@ -1200,7 +1202,8 @@ namespace {
 nmt_status score_step(nmt_model* m, const nmt_source* src, int32_t B, const float* pool, int32_t pool_rows,
                       const int32_t* state_row, const int32_t* d_y_prev, const int32_t* d_sent_id, Requests rq,
                       float* d_logp, float* d_s_new, float* d_logZ, void* d_workspace, size_t ws_bytes, hipStream_t st,
-                      float* d_alpha, float* d_c, float* d_s1, float* d_t, const AttnGroups* pre_grp = nullptr) {
+                      float* d_alpha, float* d_c, float* d_s1, float* d_t, const AttnGroups* pre_grp = nullptr,
+                      bool readouts_only = false) {
   const WsLayout L = ws_layout(m, B);
   if (!d_workspace || ((uintptr_t)d_workspace & 255)) return fail(NMT_EINVAL, "workspace must be 256-byte aligned");
   if (ws_bytes < L.total) return fail(NMT_EWORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, L.total);
@@ -1240,7 +1243,8 @@ nmt_status score_step(nmt_model* m, const nmt_source* src, int32_t B, const floa
     sg.bf16 = b16 ? 1 : 0;
     return sg;
   };
-  float* t = (float*)(ws + L.t);
+  // (the readouts of an fp32 step that ends with them go straight to the caller)
+  float* t = readouts_only && !m->bf16 ? d_t : (float*)(ws + L.t);
   float2* part = (float2*)(ws + L.part);
   ASeg h_seg = make_seg(pool, H, H, 1, m->kc);             // H_{i-1}: input states, gathered by row
   h_seg.gather = state_row;
@@ -1390,6 +1394,14 @@ nmt_status score_step(nmt_model* m, const nmt_source* src, int32_t B, const floa
   }
   mark(NMT_PHASE_READOUT + 1);
   }
+  if (readouts_only) {
+    mark(NMT_PHASE_VOCAB + 1);
+    mark(NMT_PHASE_COMBINE + 1);
+    if (e == hipSuccess && m->bf16) e = launch_bf16_to_f32(t, B, E, bf16_row(E), d_t, st);
+    if (e == hipSuccess)
+      e = launch_readout_ids(B, E, d_y_prev, V, d_sent_id, src->S, state_row, pool_rows, d_t, m->err, st);
+    return e == hipSuccess ? ok() : hip_fail(e, "nmt_step_readouts");
+  }
   // vocabulary projection with an online log-sum-exp per slice, then the combine
   // rows with one request: the vocabulary kernel also picks out its logit
   float* zreq = rq.req ? (float*)(ws + L.zreq) : nullptr;
@@ -1473,6 +1485,49 @@ nmt_status nmt_score_forest_step(nmt_model* m, const nmt_source* src, int32_t B,
   Requests rq{d_req_off, d_req, nreq, d_state_row, pool_rows};
   return score_step(m, src, B, d_state_pool, pool_rows, d_state_row, d_y_prev, d_sent_id, rq, d_logp, d_s_new, d_logZ,
                     d_workspace, ws_bytes, (hipStream_t)stream, nullptr, nullptr, nullptr, nullptr);
+}
+
+// -------------------------------------------------------- drafted words
+
+nmt_status nmt_step_readouts(nmt_model* m, const nmt_source* src, int32_t B, const float* d_state_pool,
+                             int32_t pool_rows, const int32_t* d_state_row, const int32_t* d_y_prev,
+                             const int32_t* d_sent_id, float* d_s_new, float* d_t, void* d_workspace, size_t ws_bytes,
+                             void* stream) {
+  if (!m || !src) return fail(NMT_EINVAL, "NULL model or source");
+  if (B < 0 || pool_rows < 0) return fail(NMT_EINVAL, "negative size");
+  if (B == 0) return ok();
+  if (!d_state_pool || !d_y_prev || !d_sent_id || !d_s_new || !d_t)
+    return fail(NMT_EINVAL, "a required device pointer is NULL");
+  if (!aligned16(d_state_pool) || !aligned16(d_s_new) || !aligned16(d_t))
+    return fail(NMT_EINVAL, "d_state_pool, d_s_new and d_t must be 16-byte aligned");
+  if (!d_state_row && pool_rows < B) return fail(NMT_EINVAL, "pool_rows = %d holds no state for every row of %d", pool_rows, B);
+  return score_step(m, src, B, d_state_pool, d_state_row ? pool_rows : B, d_state_row, d_y_prev, d_sent_id, Requests{},
+                    nullptr, d_s_new, nullptr, d_workspace, ws_bytes, (hipStream_t)stream, nullptr, nullptr, nullptr, d_t,
+                    nullptr, true);
+}
+
+nmt_status nmt_logits(nmt_model* m, int32_t M, const float* d_t, float* d_logits, int64_t ld_logits, float* d_logZ,
+                      void* d_workspace, size_t ws_bytes, void* stream) {
+  if (!m) return fail(NMT_EINVAL, "NULL model");
+  if (M < 0) return fail(NMT_EINVAL, "M must be >= 0 (got %d)", M);
+  if (M == 0) return ok();
+  if (!d_t || !d_logits) return fail(NMT_EINVAL, "a required device pointer is NULL");
+  if (!aligned16(d_t)) return fail(NMT_EINVAL, "d_t must be 16-byte aligned");
+  if ((uintptr_t)d_logits & 3) return fail(NMT_EINVAL, "d_logits must be 4-byte aligned");
+  const nmt_dims& d = m->dims;
+  if (ld_logits < d.V) return fail(NMT_EINVAL, "ld_logits = %lld is below V = %d", (long long)ld_logits, d.V);
+  const WsLayout L = ws_layout(m, M);
+  if (!d_workspace || ((uintptr_t)d_workspace & 255)) return fail(NMT_EINVAL, "workspace must be 256-byte aligned");
+  if (ws_bytes < L.total) return fail(NMT_EWORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, L.total);
+  nmt_status rc = check_device(m);
+  if (rc != NMT_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  float2* part = (float2*)((char*)d_workspace + L.part);
+  hipError_t e = m->out.sp.d ? launch_logits_sp(d_t, M, d.E, m->out.sp, d.V, part, L.nS, L.vtm, d_logits, ld_logits, st)
+                             : launch_vocab_logits(d_t, M, d.E, m->out, d.V, part, L.nS, L.vtm, d_logits, ld_logits, st);
+  if (e == hipSuccess && d_logZ) e = launch_logits_lse(M, part, L.nS, d_logZ, st);
+  if (e != hipSuccess) return hip_fail(e, "nmt_logits");
+  return ok();
 }
 
 // ------------------------------------------------------ several models
@@ -1661,9 +1716,15 @@ nmt_status nmt_score_ensemble(int32_t K, nmt_model* const* models, const nmt_sou
 
 }  // extern "C"
 
-// Entry points for forest.hip.
+// Entry points for forest.hip, w4.hip and verify.hip.
 namespace nmt {
 nmt_status forest_fail(nmt_status st, const char* msg) { return fail(st, "%s", msg); }
+nmt_status entry_fail(nmt_status st, const char* msg) { return fail(st, "%s", msg); }
+nmt_status entry_hip_fail(hipError_t e, const char* what) { return hip_fail(e, what); }
+nmt_status entry_ok() { return ok(); }
+nmt_status entry_check_device(const nmt_model* m) { return check_device(m); }
+OutputLayer output_layer(const nmt_model* m) { return OutputLayer{&m->out, m->dims.E, m->dims.V, m->device}; }
+int* error_flag(nmt_model* m) { return m->err; }
 }  // namespace nmt
 
 nmt_status nmt_internal_score_step(nmt_model* m, const nmt_source* src, int32_t B, const float* pool,
@@ -1707,7 +1768,8 @@ nmt_status nmt_stream_status(nmt_model* m, void* stream) {
   e = hipMemcpy(&flag, m->err, sizeof(int), hipMemcpyDeviceToHost);
   if (e == hipSuccess && flag) e = hipMemset(m->err, 0, sizeof(int));
   if (e != hipSuccess) return hip_fail(e, "nmt_stream_status");
-  if (flag) return fail(NMT_ERANGE, "an id was out of range in a call since the last status check");
+  if (flag & 1) return fail(NMT_ERANGE, "an id was out of range in a call since the last status check");
+  if (flag) return fail(NMT_ERANGE, "a row of logits was no distribution in a call since the last status check");
   return ok();
 }
 

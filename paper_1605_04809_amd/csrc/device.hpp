@@ -567,4 +567,23 @@ __device__ __forceinline__ float gru_cell(float sr, float sz, float sni, float s
 // Row of accumulator register r for lane half h.
 __device__ __forceinline__ int acc_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
+// Four floats at any 4-byte aligned address, as one access.
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
+// One lane's logits of a row: accumulator register r is vocabulary row
+// n0 + acc_row(r, h); those below V go to z.
+__device__ __forceinline__ void store_logits(float* __restrict__ z, const f32x16& acc, int n0, int h, int V) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int n = n0 + 8 * q + 4 * h;
+    if (n + 4 <= V) {
+      *(f32x4u*)(z + n) = f32x4u{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (n + e < V) z[n + e] = acc[4 * q + e];
+    }
+  }
+}
+
 }  // namespace nmt

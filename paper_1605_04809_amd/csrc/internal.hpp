@@ -63,6 +63,7 @@ constexpr int kVocabSpare = 32;                 // zero columns past the last bl
 struct SplitW {
   void* d = nullptr;
   float* bias = nullptr;  // output weights: the bias times 2^(scale + kSplitReadout), one per column
+  int bias_room = 0;      // output weights: that bias times 2^bias_room is finite (at most kSplitBiasRoom)
   int64_t blocks = 0;     // 32-column blocks (GRU: r, z, candidate of 32 units each)
   int K = 0, steps = 0;   // rows of the matrix, and 16-k steps they are padded to
   int scale = 0;
@@ -186,6 +187,14 @@ inline __host__ __device__ int bf16_row(int E) { return (E + 7) / 8 * 8; }
 hipError_t launch_vocab_lse(const float* t, int t16, int M, int E, const Packed& W, int V, float2* part, int nS,
                             int tm, const int32_t* req1, const int32_t* req_off, int nreq, float* zreq,
                             hipStream_t st);
+// The same projection for its logits: row i's V logits go to z + i * ld, and
+// the partials to part as above (launch_logits_lse merges them).
+hipError_t launch_vocab_logits(const float* t, int M, int E, const Packed& W, int V, float2* part, int nS, int tm,
+                               float* z, int64_t ld, hipStream_t st);
+hipError_t launch_logits_lse(int M, const float2* part, int nS, float* logZ, hipStream_t st);
+// Rows whose ids are out of range: NaN readouts, and the error flag.
+hipError_t launch_readout_ids(int B, int E, const int32_t* y_prev, int V, const int32_t* sent_id, int S,
+                              const int32_t* state_row, int pool_rows, float* t, int* err, hipStream_t st);
 // Requests of row b: req[req_off[b] .. req_off[b+1]) with logp at the same
 // indices (req_off nullable: one request per row, req[b] -> logp[b]).  The
 // combine takes the logits of rows with one request from zreq (the
@@ -289,6 +298,7 @@ struct SpA {
   float most, least;
 };
 constexpr int kSplitReadout = 14;  // activations' scale: tanh readouts (at most 1)
+constexpr int kSplitBiasRoom = 24;
 // states and annotations (at most 1 from the model; a row whose largest is in [2^-12, 16) stays on the halves)
 constexpr int kSplitState = 12;
 constexpr int kSpLongK = 256;      // K from which the tile GEMM splits K between wave groups
@@ -329,6 +339,9 @@ void split_vocab_shape(int M, int V, int cus, int* tm, int* nS);
 bool split_vocab_fits(int E, int64_t blocks);
 hipError_t launch_vocab_sp(const float* t, int M, int E, const SplitW& W, int V, float2* part, int nS, int tm,
                            const int32_t* req1, const int32_t* req_off, int nreq, float* zreq, hipStream_t st);
+// And launch_vocab_logits' (readouts of any magnitude: each row has a scale of its own).
+hipError_t launch_logits_sp(const float* t, int M, int E, const SplitW& W, int V, float2* part, int nS, int tm,
+                            float* z, int64_t ld, hipStream_t st);
 
 // The encoder's recurrence as one cooperative launch (encode.hip): the
 // recurrent weights of both directions in its packing (hb: units per packed

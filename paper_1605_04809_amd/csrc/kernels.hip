@@ -1149,14 +1149,18 @@ struct VocabTune {
 // or bias row reaches it: fp32 with E + nb <= Kpad - 8), so its MFMAs, which
 // would only add zeros, are skipped; its loads stay, keeping the ring's
 // schedule.  With E = 500 that is 1 of 64 k groups.
-template <class P, int VPF, bool PAD_LAST = false, int VTM_ = VocabTune<P>::VTM>
+//
+// OUT: the kernel of nmt_logits, which also writes each logit to zout (row
+// stride ldz).
+template <class P, int VPF, bool PAD_LAST = false, int VTM_ = VocabTune<P>::VTM, bool OUT = false>
 __global__ __launch_bounds__(VocabTune<P>::VNW * 64) void k_vocab_lse(const float* __restrict__ t, int t16, int M, int E,
                                                                       int nb, int Kpad, const f32x4* __restrict__ Wp,
                                                                       int64_t Npad, int V, int nM, int nS,
                                                                       float2* __restrict__ part,
                                                                       const int32_t* __restrict__ req1,
                                                                       const int32_t* __restrict__ req_off, int nreq,
-                                                                      float* __restrict__ zreq) {
+                                                                      float* __restrict__ zreq,
+                                                                      float* __restrict__ zout, int64_t ldz) {
   constexpr int VTM = VTM_, VNW = VocabTune<P>::VNW, VFN = VocabTune<P>::VFN;
   constexpr int FM = VTM / 32;
   __shared__ f32x4 As[VQMAX];
@@ -1344,6 +1348,15 @@ __global__ __launch_bounds__(VocabTune<P>::VNW * 64) void k_vocab_lse(const floa
     // group with columns past V or missing blocks (only at the end of a
     // slice) masks them out; the test is uniform over the wave.
     const int cb0 = cb_begin + gcur * VFN;
+    if constexpr (OUT) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int row = m0 + 32 * i + l32;
+#pragma unroll
+        for (int f = 0; f < VFN; ++f)
+          if (row < M && cb0 + f < cb_end) store_logits(zout + (int64_t)row * ldz, acc[i][f], (cb0 + f) * 32, h, V);
+      }
+    }
     if ((cb0 + VFN) * 32 > V || cb0 + VFN > cb_end) {
 #pragma unroll
       for (int f = 0; f < VFN; ++f)
@@ -1392,13 +1405,18 @@ __global__ __launch_bounds__(VocabTune<P>::VNW * 64) void k_vocab_lse(const floa
       const bool none = mn == -INFINITY;  // nothing but masked logits so far
       const float sc = none ? 1.f : __builtin_amdgcn_exp2f((run_m[i] - mn) * kLog2e);
       const float nm = none ? 0.f : -mn * kLog2e;
+      // (OUT: readouts of any size, whose logits' product with log2 e would round by more than 1)
+      auto fold_exp = [&](float z) {
+        if constexpr (OUT) return __builtin_amdgcn_exp2f((z - (none ? 0.f : mn)) * kLog2e);
+        return __builtin_amdgcn_exp2f(fmaf(z, kLog2e, nm));
+      };
       float s0 = 0.f, s1 = 0.f;
 #pragma unroll
       for (int f = 0; f < VFN; ++f)
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
-          s0 += __builtin_amdgcn_exp2f(fmaf(acc[i][f][r], kLog2e, nm));
-          s1 += __builtin_amdgcn_exp2f(fmaf(acc[i][f][r + 1], kLog2e, nm));
+          s0 += fold_exp(acc[i][f][r]);
+          s1 += fold_exp(acc[i][f][r + 1]);
         }
       run_s[i] = fmaf(run_s[i], sc, s0 + s1);
       run_m[i] = mn;
@@ -1513,63 +1531,71 @@ int vocab_max_kpad(bool bf16) {
   return bf16 ? VQMAX / VocabTune<PrecBF16>::VTM * PrecBF16::KV : VQMAX / VocabTune<PrecF32>::VTM * PrecF32::KV;
 }
 
-template <class P>
+template <class P, bool OUT>
 hipError_t vocab_lse(const float* t, int t16, int M, int E, const Packed& W, int V, float2* part, int nS, int tm,
-                     const int32_t* req1, const int32_t* req_off, int nreq, float* zreq, hipStream_t st) {
+                     const int32_t* req1, const int32_t* req_off, int nreq, float* zreq, float* z, int64_t ld,
+                     hipStream_t st) {
   const int nkg = (int)(W.Kpad / (2 * P::KV));
   const f32x4* Wp = (const f32x4*)W.d;
+  constexpr int PF = VocabTune<P>::VPF_MAX, TM = VocabTune<P>::VTM;
+  auto run = [&](auto vpf, auto pad, auto vtm) {
+    const int nM = ceil_div(M, decltype(vtm)::value);
+    hipLaunchKernelGGL((k_vocab_lse<P, decltype(vpf)::value, decltype(pad)::value, decltype(vtm)::value, OUT>),
+                       dim3((unsigned)(nS / 8 * 8 * nM)), dim3(VocabTune<P>::VNW * 64), 0, st, t, t16, M, E, W.nbias,
+                       (int)W.Kpad, Wp, W.Npad, V, nM, nS, part, req1, req_off, nreq, zreq, z, ld);
+  };
+  constexpr std::integral_constant<int, TM> T{};
   if constexpr (!P::kBF16) {
     if (tm == kVocabSmallTM) {
-      const int nM = ceil_div(M, kVocabSmallTM);
-      hipLaunchKernelGGL((k_vocab_lse<P, kVocabSmallVPF, true, kVocabSmallTM>), dim3((unsigned)(nS / 8 * 8 * nM)),
-                         dim3(VocabTune<P>::VNW * 64), 0, st, t, t16, M, E, W.nbias, (int)W.Kpad, Wp, W.Npad, V, nM,
-                         nS, part, req1, req_off, nreq, zreq);
+      run(std::integral_constant<int, kVocabSmallVPF>{}, std::true_type{}, std::integral_constant<int, kVocabSmallTM>{});
       return hipGetLastError();
     }
   }
-  const int nM = ceil_div(M, VocabTune<P>::VTM);
-  dim3 grid((unsigned)(nS / 8 * 8 * nM)), block(VocabTune<P>::VNW * 64);
-  constexpr int PF = VocabTune<P>::VPF_MAX;
   // the deepest prefetch that divides the k groups into at least two blocks
   auto fits = [&](int vpf) { return PF >= vpf && nkg % vpf == 0 && nkg >= 2 * vpf; };
   // the last k group only padding (see PAD_LAST; taken with the deepest prefetch)
   const bool pad_last = !P::kBF16 && E + W.nbias <= W.Kpad - 2 * P::KV;
   if (fits(16) && pad_last)
-    hipLaunchKernelGGL((k_vocab_lse<P, (PF >= 16 ? 16 : 2), !P::kBF16>), grid, block, 0, st, t, t16, M, E, W.nbias,
-                       (int)W.Kpad, Wp, W.Npad, V, nM, nS, part, req1, req_off, nreq, zreq);
+    run(std::integral_constant<int, (PF >= 16 ? 16 : 2)>{}, std::bool_constant<!P::kBF16>{}, T);
   else if (fits(16))
-    hipLaunchKernelGGL((k_vocab_lse<P, (PF >= 16 ? 16 : 2)>), grid, block, 0, st, t, t16, M, E, W.nbias, (int)W.Kpad, Wp,
-                       W.Npad, V, nM, nS, part, req1, req_off, nreq, zreq);
+    run(std::integral_constant<int, (PF >= 16 ? 16 : 2)>{}, std::false_type{}, T);
   else if (fits(8))
-    hipLaunchKernelGGL((k_vocab_lse<P, (PF >= 8 ? 8 : 2)>), grid, block, 0, st, t, t16, M, E, W.nbias, (int)W.Kpad, Wp,
-                       W.Npad, V, nM, nS, part, req1, req_off, nreq, zreq);
+    run(std::integral_constant<int, (PF >= 8 ? 8 : 2)>{}, std::false_type{}, T);
   else if (fits(4))
-    hipLaunchKernelGGL((k_vocab_lse<P, 4>), grid, block, 0, st, t, t16, M, E, W.nbias, (int)W.Kpad, Wp, W.Npad, V, nM, nS,
-                       part, req1, req_off, nreq, zreq);
+    run(std::integral_constant<int, 4>{}, std::false_type{}, T);
   else if (fits(2))
-    hipLaunchKernelGGL((k_vocab_lse<P, 2>), grid, block, 0, st, t, t16, M, E, W.nbias, (int)W.Kpad, Wp, W.Npad, V, nM, nS,
-                       part, req1, req_off, nreq, zreq);
+    run(std::integral_constant<int, 2>{}, std::false_type{}, T);
   else
     return hipErrorInvalidValue;
   return hipGetLastError();
+}
+
+// The launch's own conditions: the small tile only where its form exists (see
+// vocab_tm), and a matrix packed for the kernel.
+static bool vocab_takes(const Packed& W, int E, int V, int tm) {
+  const int64_t nkg = W.Kpad / (2 * (W.bf16 ? PrecBF16::KV : PrecF32::KV));
+  if (tm == kVocabSmallTM && (W.bf16 || nkg % kVocabSmallVPF || nkg < 2 * kVocabSmallVPF ||
+                              E + W.nbias > W.Kpad - 2 * PrecF32::KV))
+    return false;
+  return W.Kpad <= vocab_max_kpad(W.bf16) && W.Krows == E && W.nbias >= 1 &&
+         W.Npad >= ((int64_t)V + 31) / 32 * 32 + 32 && vocab_offsets_fit(W.Kpad, W.Npad, W.bf16);
 }
 
 hipError_t launch_vocab_lse(const float* t, int t16, int M, int E, const Packed& W, int V, float2* part, int nS,
                             int tm, const int32_t* req1, const int32_t* req_off, int nreq, float* zreq,
                             hipStream_t st) {
   if (M <= 0) return hipSuccess;
-  if (t16 && !W.bf16) return hipErrorInvalidValue;
-  // the small tile only where its form exists (see vocab_tm)
-  const int64_t nkg = W.Kpad / (2 * (W.bf16 ? PrecBF16::KV : PrecF32::KV));
-  if (tm == kVocabSmallTM && (W.bf16 || nkg % kVocabSmallVPF || nkg < 2 * kVocabSmallVPF ||
-                              E + W.nbias > W.Kpad - 2 * PrecF32::KV))
-    return hipErrorInvalidValue;
-  if (W.Kpad > vocab_max_kpad(W.bf16) || W.Krows != E || W.nbias < 1 || W.Npad < ((int64_t)V + 31) / 32 * 32 + 32)
-    return hipErrorInvalidValue;
-  if (!vocab_offsets_fit(W.Kpad, W.Npad, W.bf16)) return hipErrorInvalidValue;
-  if (req1 && !zreq) return hipErrorInvalidValue;
-  return W.bf16 ? vocab_lse<PrecBF16>(t, t16, M, E, W, V, part, nS, tm, req1, req_off, nreq, zreq, st)
-                : vocab_lse<PrecF32>(t, 0, M, E, W, V, part, nS, tm, req1, req_off, nreq, zreq, st);
+  if ((t16 && !W.bf16) || !vocab_takes(W, E, V, tm) || (req1 && !zreq)) return hipErrorInvalidValue;
+  return W.bf16 ? vocab_lse<PrecBF16, false>(t, t16, M, E, W, V, part, nS, tm, req1, req_off, nreq, zreq, nullptr, 0, st)
+                : vocab_lse<PrecF32, false>(t, 0, M, E, W, V, part, nS, tm, req1, req_off, nreq, zreq, nullptr, 0, st);
+}
+
+hipError_t launch_vocab_logits(const float* t, int M, int E, const Packed& W, int V, float2* part, int nS, int tm,
+                               float* z, int64_t ld, hipStream_t st) {
+  if (M <= 0) return hipSuccess;
+  if (!z || ld < V || !vocab_takes(W, E, V, tm)) return hipErrorInvalidValue;
+  return W.bf16 ? vocab_lse<PrecBF16, true>(t, 0, M, E, W, V, part, nS, tm, nullptr, nullptr, 0, nullptr, z, ld, st)
+                : vocab_lse<PrecF32, true>(t, 0, M, E, W, V, part, nS, tm, nullptr, nullptr, 0, nullptr, z, ld, st);
 }
 
 // ---------------------------------------------------- partials combine
@@ -1670,6 +1696,52 @@ hipError_t launch_lse_combine(int B, const float2* part, int nS, const float* t,
   else
     hipLaunchKernelGGL(k_lse_combine<PrecF32>, dim3(ceil_div(B, 4)), dim3(256), 0, st, B, part, nS, t, 0, E,
                        W.nbias, (int)W.Kpad, (const f32x4*)W.d, W.Npad, V, rq, y_prev, sent_id, S, logp, logZ, err, zreq);
+  return hipGetLastError();
+}
+
+// One wave per row: the slices' (max, sum) pairs merged into log Z, for a row
+// that requests nothing.
+__global__ __launch_bounds__(256) void k_logits_lse(int M, const float2* __restrict__ part, int nS,
+                                                    float* __restrict__ logZ) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= M) return;
+  float mx = -INFINITY;
+  for (int i = lane; i < nS; i += 64) mx = fmaxf(mx, part[(int64_t)i * M + row].x);
+  mx = wave_max(mx);
+  float sum = 0.f;
+  for (int i = lane; i < nS; i += 64) {
+    const float2 p = part[(int64_t)i * M + row];
+    if (p.x != -INFINITY) sum += p.y * expf(p.x - mx);
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) logZ[row] = mx + logf(sum);
+}
+
+hipError_t launch_logits_lse(int M, const float2* part, int nS, float* logZ, hipStream_t st) {
+  if (M <= 0) return hipSuccess;
+  hipLaunchKernelGGL(k_logits_lse, dim3(ceil_div(M, 4)), dim3(256), 0, st, M, part, nS, logZ);
+  return hipGetLastError();
+}
+
+// One wave per row of readouts: NaN and the error flag for a row with an id
+// out of range (k_lse_combine's checks, for a step that requests nothing).
+__global__ __launch_bounds__(256) void k_readout_ids(int B, int E, const int32_t* __restrict__ y_prev, int V,
+                                                     const int32_t* __restrict__ sent_id, int S,
+                                                     const int32_t* __restrict__ state_row, int pool_rows,
+                                                     float* __restrict__ t, int* err) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= B) return;
+  const int y = y_prev[row], s = sent_id[row], sr = state_row ? state_row[row] : 0;
+  if (y >= -1 && y < V && s >= 0 && s < S && (!state_row || (sr >= 0 && sr < pool_rows))) return;
+  for (int k = lane; k < E; k += 64) t[(int64_t)row * E + k] = __builtin_nanf("");
+  if (lane == 0) atomicOr(err, 1);
+}
+
+hipError_t launch_readout_ids(int B, int E, const int32_t* y_prev, int V, const int32_t* sent_id, int S,
+                              const int32_t* state_row, int pool_rows, float* t, int* err, hipStream_t st) {
+  if (B <= 0) return hipSuccess;
+  hipLaunchKernelGGL(k_readout_ids, dim3(ceil_div(B, 4)), dim3(256), 0, st, B, E, y_prev, V, sent_id, S, state_row,
+                     pool_rows, t, err);
   return hipGetLastError();
 }
 

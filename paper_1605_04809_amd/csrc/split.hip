@@ -839,14 +839,22 @@ hipError_t launch_plain_sp(const SpA& A, const SplitW& W, const PlainEpi& ep, in
 constexpr int kSvWaves = 8, kSvFN = 2;
 constexpr int kSvVectors = 9216;  // LDS vectors of the activation tile (144 KB)
 
-template <int VPF, int VTM>
+// OUT: the kernel of nmt_logits, which also writes each logit to zout (row
+// stride ldz) and takes readouts of any magnitude: a row is scaled by the
+// power of two that puts its largest in [2^14, 2^15), as far as its bias has
+// room in the accumulators, so it keeps 22 bits whatever its size (a tanh
+// readout's row has the fixed scale's values but for that power of two), and
+// its logits are folded in natural units.  The stores are 16 bytes a lane, a
+// 128-byte line of a row per column block over four instructions.
+template <int VPF, int VTM, bool OUT = false>
 __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restrict__ t, int M, int E, int NK,
                                                             const char* __restrict__ Wp, int64_t wbytes,
                                                             const float* __restrict__ bias, int V, int nM, int nS,
                                                             float ascale, float inv, float2* __restrict__ part,
                                                             const int32_t* __restrict__ req1,
                                                             const int32_t* __restrict__ req_off, int nreq,
-                                                            float* __restrict__ zreq) {
+                                                            float* __restrict__ zreq, float* __restrict__ zout,
+                                                            int64_t ldz, int wscale, int bias_room) {
   constexpr int VNW = kSvWaves, VFN = kSvFN, FM = VTM / 32;
   __shared__ f32x4 As[kSvVectors * VTM / 64];  // [step][half][hi, lo][row]
   __shared__ float2 red[VNW][VTM];
@@ -859,7 +867,7 @@ __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restr
   const int NB = (V + 31) / 32;
   const int cb_begin = (int)((int64_t)NB * slice / nS), cb_end = (int)((int64_t)NB * (slice + 1) / nS);
   const int ngrp = (cb_end - cb_begin + VFN - 1) / VFN;
-  const float kz = kLog2e * inv;  // the fold's exponents in the accumulators' units
+  const float kz = OUT ? kLog2e : kLog2e * inv;  // the fold's exponents in the accumulators' units
 
   float run_m[FM], run_s[FM];
 #pragma unroll
@@ -913,6 +921,42 @@ __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restr
 #pragma unroll
   for (int p = 0; p < VPF; ++p) load(ring[p], sbase + p * 2048);
 
+  int row_e[FM];      // OUT: the rows' exponents of scale, beyond kSplitReadout
+  float row_b[FM];    // and what their bias enters with
+  int stage_e = 0;    // of the row this thread stages
+  if constexpr (OUT) {
+    static_assert(VNW * 64 % VTM == 0, "a thread stages one row");
+    constexpr int SH = VNW * 64 / VTM;  // threads sharing a row
+    float* rmax = (float*)&red[0][0];   // [SH][VTM]
+    const int m = threadIdx.x % VTM, row = m0 + m;
+    float mx = 0.f;
+    if (row < M) {
+      const float* r = t + (int64_t)row * E;
+      for (int k = 4 * (threadIdx.x / VTM); k < E; k += 4 * SH) {
+        const f32x4 x = *(const f32x4*)(r + k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float a = fabsf(x[e]);
+          mx = a < INFINITY ? fmaxf(mx, a) : mx;
+        }
+      }
+    }
+    rmax[threadIdx.x] = mx;
+    __syncthreads();
+    auto row_scale = [&](int mm) {
+      float r = 0.f;
+#pragma unroll
+      for (int s = 0; s < SH; ++s) r = fmaxf(r, rmax[s * VTM + mm]);
+      const int e = r > 0.f ? -__builtin_amdgcn_frexp_expf(r) + 1 : 0;  // r = f 2^(1 - e), f in [1/2, 1)
+      return e < bias_room ? e : bias_room;
+    };
+    stage_e = row_scale(m);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      row_e[i] = row_scale(32 * i + l32);
+      row_b[i] = __builtin_amdgcn_ldexpf(1.f, row_e[i]);
+    }
+  }
   for (int idx = threadIdx.x; idx < 2 * NK * VTM; idx += VNW * 64) {
     const int m = idx % VTM, v = idx / VTM, row = m0 + m, k = 8 * v;
     f32x4 x0 = zero4(), x1 = zero4();
@@ -920,6 +964,13 @@ __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restr
       const float* r = t + (int64_t)row * E;
       if (k < E) x0 = *(const f32x4*)(r + k);
       if (k + 4 < E) x1 = *(const f32x4*)(r + k + 4);
+    }
+    if constexpr (OUT) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x0[e] = __builtin_amdgcn_ldexpf(x0[e], stage_e);
+        x1[e] = __builtin_amdgcn_ldexpf(x1[e], stage_e);
+      }
     }
     f32x4 hi, lo;
     split8(x0, x1, ascale, hi, lo);
@@ -943,7 +994,8 @@ __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restr
 #pragma unroll
     for (int f = 0; f < VFN; ++f)
 #pragma unroll
-      for (int i = 0; i < FM; ++i) acc[i][f] = __builtin_amdgcn_mfma_f32_32x32x2f32(bnext[f], 1.f, f32x16{}, 0, 0, 0);
+      for (int i = 0; i < FM; ++i)
+        acc[i][f] = __builtin_amdgcn_mfma_f32_32x32x2f32(bnext[f], OUT ? row_b[i] : 1.f, f32x16{}, 0, 0, 0);
     load_bias(bnext, gbase(gcur + VNW));
     auto kstep = [&](const f32x4* ablk, auto pc, auto last_blk, int soff) {
       constexpr int p = decltype(pc)::value;
@@ -1000,6 +1052,19 @@ __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restr
     sbase = nbase;
 
     const int cb0 = cb_begin + gcur * VFN;
+    if constexpr (OUT) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int f = 0; f < VFN; ++f) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            acc[i][f][r] = __builtin_amdgcn_ldexpf(acc[i][f][r], -(kSplitReadout + wscale + row_e[i]));
+          const int row = m0 + 32 * i + l32;
+          if (row < M && cb0 + f < cb_end) store_logits(zout + (int64_t)row * ldz, acc[i][f], (cb0 + f) * 32, h, V);
+        }
+      }
+    }
     if ((cb0 + VFN) * 32 > V || cb0 + VFN > cb_end) {
 #pragma unroll
       for (int f = 0; f < VFN; ++f)
@@ -1039,13 +1104,18 @@ __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restr
       const bool none = mn == -INFINITY;
       const float sc = none ? 1.f : __builtin_amdgcn_exp2f((run_m[i] - mn) * kz);
       const float nm = none ? 0.f : -mn * kz;
+      // (OUT: readouts of any size, whose logits' product with log2 e would round by more than 1)
+      auto fold_exp = [&](float z) {
+        if constexpr (OUT) return __builtin_amdgcn_exp2f((z - (none ? 0.f : mn)) * kLog2e);
+        return __builtin_amdgcn_exp2f(fmaf(z, kz, nm));
+      };
       float s0 = 0.f, s1 = 0.f;
 #pragma unroll
       for (int f = 0; f < VFN; ++f)
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
-          s0 += __builtin_amdgcn_exp2f(fmaf(acc[i][f][r], kz, nm));
-          s1 += __builtin_amdgcn_exp2f(fmaf(acc[i][f][r + 1], kz, nm));
+          s0 += fold_exp(acc[i][f][r]);
+          s1 += fold_exp(acc[i][f][r + 1]);
         }
       run_s[i] = fmaf(run_s[i], sc, s0 + s1);
       run_m[i] = mn;
@@ -1075,7 +1145,7 @@ __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restr
         if (mw != -INFINITY) s += red[w][rl].y * __builtin_amdgcn_exp2f((mw - mx) * kz);
       }
     }
-    if (row < M) part[(int64_t)slice * M + row] = float2{mx * inv, s};
+    if (row < M) part[(int64_t)slice * M + row] = float2{OUT ? mx : mx * inv, s};
   }
 }
 
@@ -1114,8 +1184,10 @@ bool split_vocab_fits(int E, int64_t blocks) {
   return 4 * nk * 64 <= kSvVectors && split_bytes(blocks, nk) < ((int64_t)1 << 31);
 }
 
-hipError_t launch_vocab_sp(const float* t, int M, int E, const SplitW& W, int V, float2* part, int nS, int tm,
-                           const int32_t* req1, const int32_t* req_off, int nreq, float* zreq, hipStream_t st) {
+template <bool OUT>
+static hipError_t vocab_sp(const float* t, int M, int E, const SplitW& W, int V, float2* part, int nS, int tm,
+                           const int32_t* req1, const int32_t* req_off, int nreq, float* zreq, float* z, int64_t ld,
+                           hipStream_t st) {
   if (M <= 0) return hipSuccess;
   if (!W.d || !W.bias || W.steps != split_steps(E, true) || 4 * W.steps * 64 > kSvVectors || E % 4 ||
       W.blocks < (V + 31) / 32 + 1 || (req1 && !zreq) || nS % 8 || nS < 8)
@@ -1125,8 +1197,9 @@ hipError_t launch_vocab_sp(const float* t, int M, int E, const SplitW& W, int V,
   const dim3 grid((unsigned)(nS * nM)), block(kSvWaves * 64);
   const int64_t bytes = split_bytes(W.blocks, W.steps);
   auto run = [&](auto vpf, auto vtm) {
-    hipLaunchKernelGGL((k_vocab_sp<decltype(vpf)::value, decltype(vtm)::value>), grid, block, 0, st, t, M, E, W.steps,
-                       (const char*)W.d, bytes, W.bias, V, nM, nS, ascale, inv, part, req1, req_off, nreq, zreq);
+    hipLaunchKernelGGL((k_vocab_sp<decltype(vpf)::value, decltype(vtm)::value, OUT>), grid, block, 0, st, t, M, E,
+                       W.steps, (const char*)W.d, bytes, W.bias, V, nM, nS, ascale, inv, part, req1, req_off, nreq,
+                       zreq, z, ld, W.scale, W.bias_room);
   };
   constexpr std::integral_constant<int, 2> I2{};
   constexpr std::integral_constant<int, 4> I4{};
@@ -1150,6 +1223,16 @@ hipError_t launch_vocab_sp(const float* t, int M, int E, const SplitW& W, int V,
     return hipErrorInvalidValue;
   }
   return hipGetLastError();
+}
+
+hipError_t launch_vocab_sp(const float* t, int M, int E, const SplitW& W, int V, float2* part, int nS, int tm,
+                           const int32_t* req1, const int32_t* req_off, int nreq, float* zreq, hipStream_t st) {
+  return vocab_sp<false>(t, M, E, W, V, part, nS, tm, req1, req_off, nreq, zreq, nullptr, 0, st);
+}
+hipError_t launch_logits_sp(const float* t, int M, int E, const SplitW& W, int V, float2* part, int nS, int tm,
+                            float* z, int64_t ld, hipStream_t st) {
+  if (!z || ld < V) return hipErrorInvalidValue;
+  return vocab_sp<true>(t, M, E, W, V, part, nS, tm, nullptr, nullptr, 0, nullptr, z, ld, st);
 }
 
 }  // namespace nmt
