@@ -12,13 +12,14 @@
 // comparison is in 64 bits: each row's sum of exponentials, the residual's
 // running sum.
 //
-// Three launches.  k_row_sums reads every row once: a wave takes 2,048 logits
-// of one row into registers, all loads in flight at once, and leaves their
-// (max, sum) pair.  k_residual judges its sequence from those pairs (each
-// block by itself, all positions at once) and sums the residual over its own
-// words, and k_next finds the word from the parts' sums.  A sequence's parts
-// are spread over the chip, so that one sequence over a large vocabulary takes
-// no longer than its share of the bandwidth; every sum has a fixed order.
+// Large vocabularies take four launches.  k_row_sums reads every row once: a
+// wave takes 2,048 logits of one row into registers, all loads in flight at
+// once, and leaves their (max, sum) pair.  k_judge merges a sequence's pairs
+// and finds where it ends.  k_residual sums what is left of the target over
+// 1,024 words a wave, and k_next finds the part, then the word, whose running
+// sum passes the random number.  Each stage is spread over the whole chip, so
+// one sequence takes no longer than its share of the bandwidth; every sum has
+// a fixed order.  Small ones take one launch, a block a sequence (k_verify_small).
 #include <type_traits>
 
 #include "draft.hpp"
@@ -28,10 +29,13 @@ using namespace nmt;
 namespace {
 
 constexpr int kPart = 2048;       // logits of a row that one wave sums
-constexpr int kWaves = 4;         // waves a block
+constexpr int kRest = 1024;       // words whose residual one wave sums
+constexpr int kWaves = 4;         // waves a block of the streaming kernels
+constexpr int kJudge = 8;         // positions a block judges at a time
+constexpr int kSmallV = 1024 * 8; // words of the one-launch form: eight a thread
 
 // A row's (or a part's) largest logit and the sum of e^(z - max).  A NaN makes
-// both NaN, and a row of nothing but -infinity has max -infinity and sum 0.
+// the max NaN, and a row of nothing but -infinity has max -infinity and sum 0.
 struct RowSum {
   double s;
   float m;
@@ -46,11 +50,11 @@ struct Verdict {
   int64_t t_row, p_row;  // (p_row -1: the target's alone)
   int32_t kept, bad;     // bad: no word follows (and which bits of the error flag)
   int32_t cut;           // without proposals: the word that p goes without (-1: none)
-  int32_t whole;         // the residual holds nothing: p itself (set by k_next)
+  int32_t whole;         // the residual holds nothing: p itself
 };
 
 struct VerifyArgs {
-  int S, n_draft, V, parts;       // parts of a row
+  int S, n_draft, V, parts, rests;  // parts of a row, and of a residual
   const int32_t *off, *draft;
   const void *target, *proposal;  // proposal null: drafts are certain
   int target16, proposal16;
@@ -70,30 +74,33 @@ __device__ __forceinline__ float logit(const void* z, int is16, int64_t i) {
   return is16 ? (float)((const __bf16*)z)[i] : ((const float*)z)[i];
 }
 
-// e^x for x <= 0 (or NaN's stand-in): 2^(x log2 e) as 2^n times the power
-// series of 2^f, |f| <= 1/2, whose eleventh-order remainder is 2.2e-13 of it.
-// 18 64-bit instructions a logit, at which the chip keeps up with its memory
-// (8 TB/s of fp32 logits).
+// e^x for x <= 0 as 2^n e^r, |r| <= ln 2 / 2, e^r by the polynomial that
+// interpolates it at the Chebyshev nodes (off by at most 1.1e-12 of it; the
+// odds that a word's border lies between a sum's true and computed value are
+// at most that times the vocabulary).  The 64-bit multiply-add and add are
+// full-rate instructions, rounding, conversions to integers and ldexp are
+// not: n comes out of an addition's low bits and goes into the result's
+// exponent by an integer addition.  Below e^-700 the bulk form gives about
+// 1e-304, which no sum next to a largest term of 1 sees (residuals drop it).
+template <bool kBulk>
 __device__ __forceinline__ double exp_neg(double x) {
-  const double t = fmax(x * 1.4426950408889634, -1100.0);
-  const double n = rint(t);
-  const double r = (t - n) * 0.6931471805599453;
-  double p = 1.0 / 3628800.0;
-  p = fma(p, r, 1.0 / 362880.0);
-  p = fma(p, r, 1.0 / 40320.0);
-  p = fma(p, r, 1.0 / 5040.0);
-  p = fma(p, r, 1.0 / 720.0);
-  p = fma(p, r, 1.0 / 120.0);
-  p = fma(p, r, 1.0 / 24.0);
-  p = fma(p, r, 1.0 / 6.0);
-  p = fma(p, r, 0.5);
+  constexpr double kShift = 6755399441055744.0;  // 1.5 * 2^52
+  const double d = fmax(x, kBulk ? -700.0 : -760.0);
+  const double t = fma(d, 1.4426950408889634, kShift);
+  const double n = t - kShift;
+  const double r = fma(n, -0.6931471805599453, d);
+  double p = 2.487569432882793e-05;
+  p = fma(p, r, 0.00019915864668440438);
+  p = fma(p, r, 0.0013888822738760763);
+  p = fma(p, r, 0.008333266102190715);
+  p = fma(p, r, 0.041666666883557954);
+  p = fma(p, r, 0.1666666689102446);
+  p = fma(p, r, 0.49999999999814065);
+  p = fma(p, r, 0.9999999999797875);
   p = fma(p, r, 1.0);
-  p = fma(p, r, 1.0);
-  return ldexp(p, (int)n);
-}
-
-__device__ __forceinline__ double prob(float z, const RowSum& r) {
-  return exp_neg((double)z - (double)r.m) / r.s;
+  const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+  if constexpr (!kBulk) return ldexp(p, k);
+  return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, p) + ((uint64_t)(uint32_t)k << 52));
 }
 
 // maximum() returns NaN if either is (fmaxf does not).
@@ -106,6 +113,16 @@ __device__ __forceinline__ float wave_maximum(float v) {
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+// Inclusive running sums over the wave's lanes.
+__device__ __forceinline__ double wave_scan(double v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double u = __shfl_up(v, o, 64);
+    if (lane >= o) v += u;
+  }
   return v;
 }
 
@@ -133,6 +150,8 @@ __device__ __forceinline__ void load8(const __bf16* z, int64_t i, int n, float (
   }
 }
 
+// ------------------------------------------------------------- row sums
+
 // The pair of one part of a row, by one wave: the n <= kPart logits at z.
 constexpr int kSteps = kPart / 512;  // eight logits a lane and step
 template <class T>
@@ -154,28 +173,28 @@ __device__ __forceinline__ RowSum part_sum(const T* z, int n) {
     for (int i = 0; i < kSteps; ++i)
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        s += exp_neg((double)x[i][e] - (double)m);
-        s1 += exp_neg((double)x[i][e + 1] - (double)m);
+        s += exp_neg<true>((double)x[i][e] - (double)m);
+        s1 += exp_neg<true>((double)x[i][e + 1] - (double)m);
       }
     s = wave_sum(s + s1);
   }
   return RowSum{s, m};
 }
 
+__device__ __forceinline__ RowSum merge(const RowSum& a, const RowSum& b) {
+  const float m = maximum(a.m, b.m);
+  if (!(m > -INFINITY && m < INFINITY)) return RowSum{0.0, m};
+  return RowSum{a.s * exp_neg<false>((double)a.m - (double)m) + b.s * exp_neg<false>((double)b.m - (double)m), m};
+}
+
 // A row's pair from its parts', by one wave.
 __device__ __forceinline__ RowSum merge_parts(const RowSum* r, int parts) {
   const int lane = threadIdx.x & 63;
-  RowSum mine{0.0, -INFINITY};
-  for (int i = lane; i < parts; i += 64) {
-    const RowSum o = r[i];
-    const float m = maximum(mine.m, o.m);
-    if (m > -INFINITY && m < INFINITY)
-      mine.s = mine.s * exp_neg((double)mine.m - (double)m) + o.s * exp_neg((double)o.m - (double)m);
-    mine.m = m;
-  }
+  RowSum mine = lane < parts ? r[lane] : RowSum{0.0, -INFINITY};
+  for (int i = lane + 64; i < parts; i += 64) mine = merge(mine, r[i]);
   const float m = wave_maximum(mine.m);
   const bool ok = m > -INFINITY && m < INFINITY;
-  return RowSum{wave_sum(ok ? mine.s * exp_neg((double)mine.m - (double)m) : 0.0), m};
+  return RowSum{wave_sum(ok ? mine.s * exp_neg<false>((double)mine.m - (double)m) : 0.0), m};
 }
 
 // One wave per part of a row.
@@ -193,170 +212,220 @@ __global__ __launch_bounds__(kWaves * 64) void k_row_sums(VerifyArgs a, int64_t 
   if ((threadIdx.x & 63) == 0) a.rows[id] = r;
 }
 
-// The verdict on sequence s by a block of kWaves waves, kWaves positions at a
-// time.  With write, log p of each draft goes out too (and every position is
-// looked at for it).
-__device__ Verdict judge(const VerifyArgs& a, int s, bool write) {
-  __shared__ Verdict sh[kWaves];
-  __shared__ int stop[kWaves];
+// --------------------------------------------------------------- verdict
+
+// The verdict on sequence s, by a block of 2 kJudge waves: kJudge positions at
+// a time, a wave for each's target row and one for its proposal row
+// (row_sum(is_target, row)), then the first wave with a lane a position.  Log p
+// of each draft goes out too, and every position is looked at for it.  The
+// block's verdict is in *out after the call.
+template <class RowSumOf>
+__device__ __forceinline__ void judge(const VerifyArgs& a, int s, int o0, int o1, Verdict* out, RowSumOf&& row_sum) {
+  __shared__ RowSum rows[2][kJudge];
+  __shared__ int done;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int o0 = a.off[s], o1 = a.off[s + 1];
-  Verdict v{};
   if (o0 < 0 || o1 < o0 || o1 > a.n_draft) {
-    v.bad = 1;
-    return v;
-  }
-  const int64_t n_target = (int64_t)a.n_draft + a.S;
-  const int n = o1 - o0;
-  bool found = false;
-  for (int j0 = 0; j0 <= n && !(found && !write); j0 += kWaves) {
-    const int j = j0 + wave;
-    if (j <= n) {
-      const int64_t tr = (int64_t)o0 + s + j, pr = (int64_t)o0 + j;
-      Verdict w{};
-      w.kept = j;
-      w.t_row = tr;
-      w.p_row = -1;
-      w.cut = -1;
-      const bool has_p = j < n && a.proposal;
-      const int32_t d = j < n ? a.draft[pr] : 0;
-      const bool d_ok = d >= 0 && d < a.V;
-      const float zt = logit(a.target, a.target16, tr * a.ld_t + (d_ok ? d : 0));
-      const float zp = has_p ? logit(a.proposal, a.proposal16, pr * a.ld_p + (d_ok ? d : 0)) : 0.f;
-      w.rt = merge_parts(a.rows + tr * a.parts, a.parts);
-      if (has_p) w.rp = merge_parts(a.rows + (n_target + pr) * a.parts, a.parts);
-      const bool t_ok = is_distribution(w.rt);
-      if (!d_ok)
-        w.bad = 1;
-      else if (!t_ok || (has_p && !is_distribution(w.rp)))
-        w.bad = 2;
-      bool end = true;
-      if (j < n) {
-        if (!w.bad) {
-          const double q = has_p ? prob(zp, w.rp) : 1.0;
-          end = !((double)a.u[tr] * q < prob(zt, w.rt));  // (a NaN ends it too)
-          w.p_row = has_p ? pr : -1;
-          w.cut = has_p ? -1 : d;
-        }
-        if (write && lane == 0)
-          a.draft_logp[pr] = d_ok && t_ok ? (float)((double)zt - (double)w.rt.m - log(w.rt.s)) : __builtin_nanf("");
-      }
-      if (lane == 0) {
-        sh[wave] = w;
-        stop[wave] = end;
-      }
-    } else if (lane == 0) {
-      stop[wave] = 0;
+    if (threadIdx.x == 0) {
+      *out = Verdict{};
+      out->bad = 1;
     }
     __syncthreads();
-    for (int w = 0; w < kWaves && !found; ++w)
-      if (stop[w]) {
-        v = sh[w];
-        found = true;
-      }
-    __syncthreads();
+    return;
   }
-  return v;
+  const int n = o1 - o0;
+  if (threadIdx.x == 0) done = 0;
+  for (int j0 = 0; j0 <= n; j0 += kJudge) {
+    const bool prop = wave >= kJudge;
+    const int jw = j0 + wave % kJudge;
+    if (jw < n + (prop ? 0 : 1) && (!prop || a.proposal)) {
+      const RowSum r = row_sum(!prop, prop ? (int64_t)o0 + jw : (int64_t)o0 + s + jw);
+      if (lane == 0) rows[prop][wave % kJudge] = r;
+    }
+    // what else a position is judged by, on its way meanwhile
+    const int j = j0 + lane;
+    const bool pos = wave == 0 && lane < kJudge && j <= n, has_p = pos && j < n && a.proposal;
+    const int64_t tr = (int64_t)o0 + s + j, pr = (int64_t)o0 + j;
+    const int32_t d = pos && j < n ? a.draft[pr] : 0;
+    const float u = pos ? a.u[tr] : 0.f;
+    const bool d_ok = d >= 0 && d < a.V;
+    const float zt = pos ? logit(a.target, a.target16, tr * a.ld_t + (d_ok ? d : 0)) : 0.f;
+    const float zp = has_p ? logit(a.proposal, a.proposal16, pr * a.ld_p + (d_ok ? d : 0)) : 0.f;
+    __syncthreads();
+    if (wave == 0) {
+      const RowSum rt = rows[0][lane % kJudge], rp = has_p ? rows[1][lane % kJudge] : RowSum{1.0, 0.f};
+      const bool t_ok = is_distribution(rt);
+      const int bad = !d_ok ? 1 : !t_ok || !is_distribution(rp) ? 2 : 0;
+      const double p = exp_neg<false>((double)zt - (double)rt.m) / rt.s;
+      const double q = has_p ? exp_neg<false>((double)zp - (double)rp.m) / rp.s : 1.0;
+      const bool end = pos && (j == n || bad || !((double)u * q < p));
+      const uint64_t ends = __ballot(end);
+      if (!done && ends && lane == __builtin_ctzll(ends)) {
+        *out = Verdict{rt, rp, tr, has_p ? pr : -1, j, bad, j < n && !a.proposal ? d : -1, 0};
+        done = 1;
+      }
+      if (pos && j < n && a.draft_logp)
+        a.draft_logp[pr] = d_ok && t_ok ? (float)((double)zt - (double)rt.m - log(rt.s)) : __builtin_nanf("");
+    }
+    __syncthreads();
+    if (done && !a.draft_logp) break;
+  }
 }
 
-// What is left of word w for the draw (it, ip: the rows' sums' reciprocals).
-__device__ __forceinline__ double residual(const Verdict& v, double it, double ip, float zt, float zp, int w) {
-  double r = exp_neg((double)zt - (double)v.rt.m) * it;
-  if (v.whole) return r;
-  if (v.p_row >= 0) r -= exp_neg((double)zp - (double)v.rp.m) * ip;
-  return w == v.cut || r < 0.0 ? 0.0 : r;
+// One block a sequence.
+__global__ __launch_bounds__(2 * kJudge * 64) void k_judge(VerifyArgs a) {
+  const int s = blockIdx.x;
+  const int64_t n_target = (int64_t)a.n_draft + a.S;
+  judge(a, s, a.off[s], a.off[s + 1], a.verdict + s, [&](bool tgt, int64_t row) {
+    return merge_parts(a.rows + (tgt ? row : n_target + row) * a.parts, a.parts);
+  });
 }
+
+// A sequence that no word follows.
+__device__ __forceinline__ void write_bad(const VerifyArgs& a, int s, const Verdict& v) {
+  a.accepted[s] = v.kept;
+  a.next[s] = -1;
+  if (a.next_logp) a.next_logp[s] = __builtin_nanf("");
+  atomicOr(a.err, v.bad);
+}
+
+// -------------------------------------------------------------- residual
+
+// What is left of words w0 .. w0 + 7 for the draw (of those below w0 + n).
 template <class TT, class TP>
 __device__ __forceinline__ void residual8(const VerifyArgs& a, const Verdict& v, int w0, int n, double (&r)[8]) {
   float xt[8], xp[8];
+  const bool minus = v.p_row >= 0 && !v.whole;
   load8((const TT*)a.target, v.t_row * a.ld_t + w0, n, xt);
-  if (v.p_row >= 0) {
+  if (minus) {
     load8((const TP*)a.proposal, v.p_row * a.ld_p + w0, n, xp);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) xp[e] = 0.f;
+    for (int e = 0; e < 8; ++e) xp[e] = -INFINITY;
   }
-  const double it = 1.0 / v.rt.s, ip = v.p_row >= 0 ? 1.0 / v.rp.s : 0.0;
+  const double it = 1.0 / v.rt.s, ip = minus ? 1.0 / v.rp.s : 0.0, mp = minus ? v.rp.m : 0.0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = residual(v, it, ip, xt[e], xp[e], w0 + e);
+  for (int e = 0; e < 8; ++e) {
+    r[e] = exp_neg<true>((double)xt[e] - (double)v.rt.m) * it;
+    if (minus) r[e] -= exp_neg<true>((double)xp[e] - mp) * ip;
+    // (the bulk form's nothing is no probability)
+    if (r[e] < 1e-290 || (w0 + e == v.cut && !v.whole)) r[e] = 0.0;
+  }
 }
-// f with the two matrices' element types.
-template <class F>
-__device__ __forceinline__ void with_types(const VerifyArgs& a, F&& f) {
+__device__ __forceinline__ void residual8(const VerifyArgs& a, const Verdict& v, int w0, double (&r)[8]) {
+  const int n = a.V - w0;
   if (a.target16) {
     if (a.proposal16)
-      f((__bf16*)nullptr, (__bf16*)nullptr);
+      residual8<__bf16, __bf16>(a, v, w0, n, r);
     else
-      f((__bf16*)nullptr, (float*)nullptr);
+      residual8<__bf16, float>(a, v, w0, n, r);
   } else {
     if (a.proposal16)
-      f((float*)nullptr, (__bf16*)nullptr);
+      residual8<float, __bf16>(a, v, w0, n, r);
     else
-      f((float*)nullptr, (float*)nullptr);
+      residual8<float, float>(a, v, w0, n, r);
   }
 }
+__device__ __forceinline__ double sum8(const double (&r)[8]) {
+  return ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7]));
+}
 
-// The sum of the residual over part p of sequence s's words, by one wave.
+// The residual's sum over part p of the words, by one wave.
 __device__ __forceinline__ double rest_sum(const VerifyArgs& a, const Verdict& v, int part) {
-  const int lane = threadIdx.x & 63;
   double sum = 0.0;
-  with_types(a, [&](auto* tt, auto* tp) {
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int w0 = part * kPart + i * 512 + lane * 8;
-      double r[8];
-      residual8<std::remove_pointer_t<decltype(tt)>, std::remove_pointer_t<decltype(tp)>>(a, v, w0, a.V - w0, r);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum += r[e];
-    }
-  });
+#pragma unroll 1
+  for (int i = 0; i < kRest / 512; ++i) {
+    double r[8];
+    residual8(a, v, part * kRest + i * 512 + (threadIdx.x & 63) * 8, r);
+    sum += sum8(r);
+  }
   return wave_sum(sum);
 }
 
-// One wave per part of a sequence's words, kWaves parts a block: the verdict
-// (written by the sequence's first block), then the residual's sums.
-__global__ __launch_bounds__(kWaves * 64) void k_residual(VerifyArgs a, int blocks) {
-  const int s = blockIdx.x / blocks, b = blockIdx.x % blocks;
-  const Verdict v = judge(a, s, b == 0 && a.draft_logp);
-  if (b == 0 && threadIdx.x == 0) a.verdict[s] = v;
-  const int part = b * kWaves + (threadIdx.x >> 6);
-  if (v.bad || part >= a.parts) return;
-  const double sum = rest_sum(a, v, part);
-  if ((threadIdx.x & 63) == 0) a.rest[(int64_t)s * a.parts + part] = sum;
+// One wave per part of a sequence's words.
+__global__ __launch_bounds__(kWaves * 64) void k_residual(VerifyArgs a, int64_t n_all) {
+  const int64_t id = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (id >= n_all) return;
+  const int s = (int)(id / a.rests);
+  const Verdict v = a.verdict[s];
+  if (v.bad) return;
+  const double sum = rest_sum(a, v, (int)(id % a.rests));
+  if ((threadIdx.x & 63) == 0) a.rest[id] = sum;
 }
 
-// Inclusive running sums over the wave's lanes.
-__device__ __forceinline__ double wave_scan(double v) {
-  const int lane = threadIdx.x & 63;
+// The first word of the block's (eight a thread from w0, whose residuals are
+// r and whose running sum starts at `run`) whose running sum passes the goal;
+// where rounding has left the goal at the whole sum, the last that has any.
+template <int NW>
+__device__ __forceinline__ int pick(const double (&r)[8], double run, double goal, int w0) {
+  __shared__ int word[NW], last[NW];
+  int hit_w = 0x7fffffff, last_w = -1;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
+  for (int e = 0; e < 8; ++e) {
+    run += r[e];
+    if (r[e] > 0.0) {
+      if (run > goal && hit_w == 0x7fffffff) hit_w = w0 + e;
+      last_w = w0 + e;
+    }
   }
-  return v;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    hit_w = min(hit_w, __shfl_xor(hit_w, o, 64));
+    last_w = max(last_w, __shfl_xor(last_w, o, 64));
+  }
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    word[wave] = hit_w;
+    last[wave] = last_w;
+  }
+  __syncthreads();
+  for (int i = 0; i < NW; ++i) {
+    hit_w = min(hit_w, word[i]);
+    last_w = max(last_w, last[i]);
+  }
+  return hit_w == 0x7fffffff ? last_w : hit_w;
 }
 
-// The sequence's word: the part whose running sum passes the goal, then the
-// word within it.  One block a sequence, a wave per 512 words of the part.
-__global__ __launch_bounds__(kSteps * 64) void k_next(VerifyArgs a) {
-  __shared__ double step_sum[kSteps];
-  __shared__ int word[kSteps], last[kSteps];
+// The sum of the block's values before this thread's, and all of them.
+template <int NW>
+__device__ __forceinline__ double block_before(double mine, double* total) {
+  __shared__ double sums[NW];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const double sc = wave_scan(mine), up = __shfl_up(sc, 1, 64);
+  __syncthreads();
+  if (lane == 63) sums[wave] = sc;
+  __syncthreads();
+  double before = 0.0, sum = 0.0;
+  for (int i = 0; i < NW; ++i) {
+    if (i == wave) before = sum;
+    sum += sums[i];
+  }
+  *total = sum;
+  return before + (lane > 0 ? up : 0.0);
+}
+
+__device__ __forceinline__ void write_next(const VerifyArgs& a, int s, const Verdict& v, int w) {
+  a.accepted[s] = v.kept;
+  a.next[s] = w;
+  if (a.next_logp)
+    a.next_logp[s] = (float)((double)logit(a.target, a.target16, v.t_row * a.ld_t + w) - (double)v.rt.m - log(v.rt.s));
+}
+
+// The sequence's word from its residual's parts.  One block a sequence, eight
+// words of the part a thread.
+constexpr int kNextWaves = kRest / 512;
+__global__ __launch_bounds__(kNextWaves * 64) void k_next(VerifyArgs a) {
   const int s = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   Verdict v = a.verdict[s];
   if (v.bad) {
-    if (threadIdx.x == 0) {
-      a.accepted[s] = v.kept;
-      a.next[s] = -1;
-      if (a.next_logp) a.next_logp[s] = __builtin_nanf("");
-      atomicOr(a.err, v.bad);
-    }
+    if (threadIdx.x == 0) write_bad(a, s, v);
     return;
   }
-  double* rest = a.rest + (int64_t)s * a.parts;
+  double* rest = a.rest + (int64_t)s * a.rests;
+  const double u = a.u[(int64_t)a.off[s + 1] + s];
   auto running = [&](auto&& each) {  // each(part, its sum, the sum before it); returns the whole sum
     double sum = 0.0;
-    for (int i = 0; i < a.parts; i += 64) {
-      const double x = i + lane < a.parts ? rest[i + lane] : 0.0;
+    for (int i = 0; i < a.rests; i += 64) {
+      const double x = i + lane < a.rests ? rest[i + lane] : 0.0;
       const double sc = wave_scan(x);
       const double up = __shfl_up(sc, 1, 64);
       each(i, x, sum + (lane > 0 ? up : 0.0));
@@ -367,14 +436,14 @@ __global__ __launch_bounds__(kSteps * 64) void k_next(VerifyArgs a) {
   double total = running([](int, double, double) {});
   if (!(total > 0.0)) {  // nothing left: p itself
     v.whole = 1;
-    for (int p = wave; p < a.parts; p += kSteps) {
+    for (int p = wave; p < a.rests; p += kNextWaves) {
       const double sum = rest_sum(a, v, p);
       if (lane == 0) rest[p] = sum;
     }
     __syncthreads();
     total = running([](int, double, double) {});
   }
-  const double goal = (double)a.u[(int64_t)a.off[s + 1] + s] * total;
+  const double goal = u * total;
   int part = -1, last_part = 0;
   double before = 0.0, last_before = 0.0;
   running([&](int i, double x, double ahead) {
@@ -394,50 +463,48 @@ __global__ __launch_bounds__(kSteps * 64) void k_next(VerifyArgs a) {
     part = last_part;
     before = last_before;
   }
-  const int w0 = part * kPart + wave * 512 + lane * 8;
-  double r[8], mine = 0.0;
-  with_types(a, [&](auto* tt, auto* tp) {
-    residual8<std::remove_pointer_t<decltype(tt)>, std::remove_pointer_t<decltype(tp)>>(a, v, w0, a.V - w0, r);
+  const int w0 = part * kRest + (int)threadIdx.x * 8;
+  double r[8], all;
+  residual8(a, v, w0, r);
+  const double ahead = block_before<kNextWaves>(sum8(r), &all);
+  const int w = pick<kNextWaves>(r, before + ahead, goal, w0);
+  if (threadIdx.x == 0) write_next(a, s, v, w);
+}
+
+// ------------------------------------------------------- small vocabularies
+
+// A sequence by one block: V <= kSmallV.
+__global__ __launch_bounds__(2 * kJudge * 64) void k_verify_small(VerifyArgs a) {
+  __shared__ Verdict shared_v;
+  const int s = blockIdx.x, o0 = a.off[s], o1 = a.off[s + 1];
+  judge(a, s, o0, o1, &shared_v, [&](bool tgt, int64_t row) {
+    RowSum r{0.0, -INFINITY};
+#pragma unroll 1
+    for (int i = 0; i < a.V; i += kPart) {
+      const int n = min(kPart, a.V - i);
+      const RowSum p = (tgt ? a.target16 : a.proposal16)
+                           ? part_sum((const __bf16*)(tgt ? a.target : a.proposal) + row * (tgt ? a.ld_t : a.ld_p) + i, n)
+                           : part_sum((const float*)(tgt ? a.target : a.proposal) + row * (tgt ? a.ld_t : a.ld_p) + i, n);
+      r = i ? merge(r, p) : p;
+    }
+    return r;
   });
-#pragma unroll
-  for (int e = 0; e < 8; ++e) mine += r[e];
-  const double sc = wave_scan(mine), up = __shfl_up(sc, 1, 64);
-  if (lane == 63) step_sum[wave] = sc;
-  __syncthreads();
-  double run = before;
-  for (int w = 0; w < wave; ++w) run += step_sum[w];
-  run += lane > 0 ? up : 0.0;
-  int hit_w = a.V, last_w = -1;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    run += r[e];
-    if (r[e] > 0.0) {
-      if (run > goal && hit_w == a.V) hit_w = w0 + e;
-      last_w = w0 + e;
-    }
+  Verdict v = shared_v;
+  if (v.bad) {
+    if (threadIdx.x == 0) write_bad(a, s, v);
+    return;
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    hit_w = min(hit_w, __shfl_xor(hit_w, o, 64));
-    last_w = max(last_w, __shfl_xor(last_w, o, 64));
+  const int w0 = (int)threadIdx.x * 8;
+  double r[8], total, ahead;
+  residual8(a, v, w0, r);
+  ahead = block_before<2 * kJudge>(sum8(r), &total);
+  if (!(total > 0.0)) {  // nothing left: p itself
+    v.whole = 1;
+    residual8(a, v, w0, r);
+    ahead = block_before<2 * kJudge>(sum8(r), &total);
   }
-  if (lane == 0) {
-    word[wave] = hit_w;
-    last[wave] = last_w;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    int w = a.V, l = -1;
-    for (int i = 0; i < kSteps; ++i) {
-      w = min(w, word[i]);
-      l = max(l, last[i]);
-    }
-    if (w == a.V) w = l;
-    a.accepted[s] = v.kept;
-    a.next[s] = w;
-    if (a.next_logp)
-      a.next_logp[s] = (float)((double)logit(a.target, a.target16, v.t_row * a.ld_t + w) - (double)v.rt.m - log(v.rt.s));
-  }
+  const int w = pick<2 * kJudge>(r, ahead, (double)a.u[(int64_t)o1 + s] * total, w0);
+  if (threadIdx.x == 0) write_next(a, s, v, w);
 }
 
 // Workspace layout (offsets in bytes, 256-aligned).
@@ -445,12 +512,12 @@ struct VerifyWs {
   size_t rows, verdict, rest, total;
 };
 VerifyWs verify_ws(int V, int64_t S, int64_t n_draft) {
-  const size_t parts = (size_t)ceil_div(V, kPart);
+  const size_t parts = (size_t)ceil_div(V, kPart), rests = (size_t)ceil_div(V, kRest);
   auto al = [](size_t x) { return (x + 255) / 256 * 256; };
   VerifyWs L{};
   L.verdict = L.rows + al((size_t)(S + 2 * n_draft) * parts * sizeof(RowSum));
   L.rest = L.verdict + al((size_t)S * sizeof(Verdict));
-  L.total = L.rest + al((size_t)S * parts * sizeof(double));
+  L.total = L.rest + al((size_t)S * rests * sizeof(double));
   return L;
 }
 
@@ -481,9 +548,11 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   if (((uintptr_t)d_target & (target_type == NMT_BF16 ? 1 : 3)) ||
       ((uintptr_t)d_proposal & (proposal_type == NMT_BF16 ? 1 : 3)))
     return entry_fail(NMT_EINVAL, "logits must be aligned to their elements");
-  const int parts = ceil_div(V, kPart), res_blocks = ceil_div(parts, kWaves);
+  const int parts = ceil_div(V, kPart), rests = ceil_div(V, kRest);
   const int64_t n_rows = (int64_t)n_draft + S + (d_proposal ? n_draft : 0), n_parts = n_rows * parts;
-  if ((n_parts + kWaves - 1) / kWaves > 0x7fffffff || (int64_t)S * res_blocks > 0x7fffffff)
+  const int64_t n_rests = (int64_t)S * rests;
+  auto blocks = [](int64_t waves) { return (waves + kWaves - 1) / kWaves; };
+  if (blocks(n_parts) > 0x7fffffff || blocks(n_rests) > 0x7fffffff)
     return entry_fail(NMT_EINVAL, "too many rows of logits for one call");
   const VerifyWs L = verify_ws(V, S, n_draft);
   if (!d_workspace || ((uintptr_t)d_workspace & 255)) return entry_fail(NMT_EINVAL, "workspace must be 256-byte aligned");
@@ -491,20 +560,24 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   const nmt_status rc = entry_check_device(m);
   if (rc != NMT_OK) return rc;
   char* ws = (char*)d_workspace;
-  const VerifyArgs a{S, n_draft, V, parts, d_draft_off, d_draft, d_target, d_proposal, target_type == NMT_BF16,
+  const VerifyArgs a{S, n_draft, V, parts, rests, d_draft_off, d_draft, d_target, d_proposal, target_type == NMT_BF16,
                      proposal_type == NMT_BF16, ld_target, ld_proposal, d_u, d_accepted, d_next, d_draft_logp,
                      d_next_logp, (RowSum*)(ws + L.rows), (Verdict*)(ws + L.verdict), (double*)(ws + L.rest),
                      error_flag(m)};
   hipStream_t st = (hipStream_t)stream;
-  hipLaunchKernelGGL(k_row_sums, dim3((unsigned)((n_parts + kWaves - 1) / kWaves)), dim3(kWaves * 64), 0, st, a, n_parts);
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess) {
-    hipLaunchKernelGGL(k_residual, dim3((unsigned)(S * res_blocks)), dim3(kWaves * 64), 0, st, a, res_blocks);
+  hipError_t e = hipSuccess;
+  auto run = [&](auto* kernel, int64_t grid, int threads, auto... args) {
+    if (e != hipSuccess) return;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, st, a, args...);
     e = hipGetLastError();
-  }
-  if (e == hipSuccess) {
-    hipLaunchKernelGGL(k_next, dim3(S), dim3(kSteps * 64), 0, st, a);
-    e = hipGetLastError();
+  };
+  if (V <= kSmallV) {
+    run(k_verify_small, S, 2 * kJudge * 64);
+  } else {
+    run(k_row_sums, blocks(n_parts), kWaves * 64, n_parts);
+    run(k_judge, S, 2 * kJudge * 64);
+    run(k_residual, blocks(n_rests), kWaves * 64, n_rests);
+    run(k_next, S, kNextWaves * 64);
   }
   if (e != hipSuccess) return entry_hip_fail(e, "nmt_verify_drafts");
   return entry_ok();
