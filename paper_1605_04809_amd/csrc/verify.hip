@@ -20,8 +20,6 @@
 // sum passes the random number.  Each stage is spread over the whole chip, so
 // one sequence takes no longer than its share of the bandwidth; every sum has
 // a fixed order.  Small ones take one launch, a block a sequence (k_verify_small).
-#include <type_traits>
-
 #include "draft.hpp"
 
 using namespace nmt;
@@ -75,32 +73,26 @@ __device__ __forceinline__ float logit(const void* z, int is16, int64_t i) {
 }
 
 // e^x for x <= 0 as 2^n e^r, |r| <= ln 2 / 2, e^r by the polynomial that
-// interpolates it at the Chebyshev nodes (off by at most 1.1e-12 of it; the
-// odds that a word's border lies between a sum's true and computed value are
-// at most that times the vocabulary).  The 64-bit multiply-add and add are
-// full-rate instructions, rounding, conversions to integers and ldexp are
-// not: n comes out of an addition's low bits and goes into the result's
-// exponent by an integer addition.  Below e^-700 the bulk form gives about
-// 1e-304, which no sum next to a largest term of 1 sees (residuals drop it).
-template <bool kBulk>
+// interpolates it at the Chebyshev nodes (off by at most 5.6e-11 of it, and
+// exact at 0).  15 64-bit instructions a logit, each at the rate of a 64-bit
+// multiply-add: 2 T logits/s, which keeps up with 8 TB/s of fp32 ones.  The
+// odds that a sum's error moves a decision are its part of the distance
+// between two borders: at most 5.6e-11 for a draft, and 1e-5 even for a word
+// out of 100,000 equal ones if every error had the same sign.
 __device__ __forceinline__ double exp_neg(double x) {
-  constexpr double kShift = 6755399441055744.0;  // 1.5 * 2^52
-  const double d = fmax(x, kBulk ? -700.0 : -760.0);
+  constexpr double kShift = 6755399441055744.0;  // 1.5 * 2^52: n comes out in the sum's low bits
+  const double d = fmax(x, -760.0);
   const double t = fma(d, 1.4426950408889634, kShift);
-  const double n = t - kShift;
-  const double r = fma(n, -0.6931471805599453, d);
-  double p = 2.487569432882793e-05;
-  p = fma(p, r, 0.00019915864668440438);
-  p = fma(p, r, 0.0013888822738760763);
-  p = fma(p, r, 0.008333266102190715);
-  p = fma(p, r, 0.041666666883557954);
-  p = fma(p, r, 0.1666666689102446);
-  p = fma(p, r, 0.49999999999814065);
-  p = fma(p, r, 0.9999999999797875);
+  const double r = fma(t - kShift, -0.6931471805599453, d);
+  double p = 0.00019907567086439808;
+  p = fma(p, r, 0.0013948578255139586);
+  p = fma(p, r, 0.00833328354312129);
+  p = fma(p, r, 0.04166621832056651);
+  p = fma(p, r, 0.16666666786284912);
+  p = fma(p, r, 0.5000000107728596);
+  p = fma(p, r, 0.9999999999955115);
   p = fma(p, r, 1.0);
-  const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
-  if constexpr (!kBulk) return ldexp(p, k);
-  return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, p) + ((uint64_t)(uint32_t)k << 52));
+  return ldexp(p, (int)(uint32_t)__builtin_bit_cast(uint64_t, t));
 }
 
 // maximum() returns NaN if either is (fmaxf does not).
@@ -127,26 +119,22 @@ __device__ __forceinline__ double wave_scan(double v) {
 }
 
 // Eight consecutive logits at z[i], those from n on as -infinity; any
-// alignment of the elements' own.
+// alignment of the elements' own.  (The type is a branch here, the same for
+// the whole wave, and not a form of each kernel: their code would double, and
+// a block that runs once waits for its instructions as for its data.)
 typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
-__device__ __forceinline__ void load8(const float* z, int64_t i, int n, float (&x)[8]) {
-  if (n >= 8) {
-    const f32x4u a = *(const f32x4u*)(z + i), b = *(const f32x4u*)(z + i + 4);
+__device__ __forceinline__ void load8(const void* z, int is16, int64_t i, int n, float (&x)[8]) {
+  if (n < 8) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = e < 4 ? a[e] : b[e - 4];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = e < n ? z[i + e] : -INFINITY;
-  }
-}
-__device__ __forceinline__ void load8(const __bf16* z, int64_t i, int n, float (&x)[8]) {
-  if (n >= 8) {
-    const bf16x8u a = *(const bf16x8u*)(z + i);
+    for (int e = 0; e < 8; ++e) x[e] = e < n ? logit(z, is16, i + e) : -INFINITY;
+  } else if (is16) {
+    const bf16x8u a = *(const bf16x8u*)((const __bf16*)z + i);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (float)a[e];
   } else {
+    const f32x4u a = *(const f32x4u*)((const float*)z + i), b = *(const f32x4u*)((const float*)z + i + 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = e < n ? (float)z[i + e] : -INFINITY;
+    for (int e = 0; e < 8; ++e) x[e] = e < 4 ? a[e] : b[e - 4];
   }
 }
 
@@ -154,12 +142,17 @@ __device__ __forceinline__ void load8(const __bf16* z, int64_t i, int n, float (
 
 // The pair of one part of a row, by one wave: the n <= kPart logits at z.
 constexpr int kSteps = kPart / 512;  // eight logits a lane and step
-template <class T>
-__device__ __forceinline__ RowSum part_sum(const T* z, int n) {
+__device__ __forceinline__ RowSum part_sum(const void* z, int is16, int64_t at, int n) {
   const int lane = threadIdx.x & 63;
   float x[kSteps][8];
+  auto load = [&](int type) {
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) load8(z, i * 512 + lane * 8, n - (i * 512 + lane * 8), x[i]);
+    for (int i = 0; i < kSteps; ++i) load8(z, type, at + i * 512 + lane * 8, n - (i * 512 + lane * 8), x[i]);
+  };
+  if (is16)
+    load(1);
+  else
+    load(0);
   float m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
@@ -170,12 +163,14 @@ __device__ __forceinline__ RowSum part_sum(const T* z, int n) {
   if (m > -INFINITY && m < INFINITY) {
     double s1 = 0.0;
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
+    for (int i = 0; i < kSteps; ++i) {
+      if (i * 512 >= n) break;  // (a short row has few steps)
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        s += exp_neg<true>((double)x[i][e] - (double)m);
-        s1 += exp_neg<true>((double)x[i][e + 1] - (double)m);
+        s += exp_neg((double)x[i][e] - (double)m);
+        s1 += exp_neg((double)x[i][e + 1] - (double)m);
       }
+    }
     s = wave_sum(s + s1);
   }
   return RowSum{s, m};
@@ -184,7 +179,7 @@ __device__ __forceinline__ RowSum part_sum(const T* z, int n) {
 __device__ __forceinline__ RowSum merge(const RowSum& a, const RowSum& b) {
   const float m = maximum(a.m, b.m);
   if (!(m > -INFINITY && m < INFINITY)) return RowSum{0.0, m};
-  return RowSum{a.s * exp_neg<false>((double)a.m - (double)m) + b.s * exp_neg<false>((double)b.m - (double)m), m};
+  return RowSum{a.s * exp_neg((double)a.m - (double)m) + b.s * exp_neg((double)b.m - (double)m), m};
 }
 
 // A row's pair from its parts', by one wave.
@@ -194,7 +189,7 @@ __device__ __forceinline__ RowSum merge_parts(const RowSum* r, int parts) {
   for (int i = lane + 64; i < parts; i += 64) mine = merge(mine, r[i]);
   const float m = wave_maximum(mine.m);
   const bool ok = m > -INFINITY && m < INFINITY;
-  return RowSum{wave_sum(ok ? mine.s * exp_neg<false>((double)mine.m - (double)m) : 0.0), m};
+  return RowSum{wave_sum(ok ? mine.s * exp_neg((double)mine.m - (double)m) : 0.0), m};
 }
 
 // One wave per part of a row.
@@ -206,9 +201,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_row_sums(VerifyArgs a, int64_t 
   const int64_t n_target = (int64_t)a.n_draft + a.S;
   const bool tgt = row < n_target;
   const int64_t at = (tgt ? row * a.ld_t : (row - n_target) * a.ld_p) + (int64_t)part * kPart;
-  const void* z = tgt ? a.target : a.proposal;
-  const RowSum r = (tgt ? a.target16 : a.proposal16) ? part_sum((const __bf16*)z + at, n)
-                                                     : part_sum((const float*)z + at, n);
+  const RowSum r = part_sum(tgt ? a.target : a.proposal, tgt ? a.target16 : a.proposal16, at, n);
   if ((threadIdx.x & 63) == 0) a.rows[id] = r;
 }
 
@@ -255,8 +248,8 @@ __device__ __forceinline__ void judge(const VerifyArgs& a, int s, int o0, int o1
       const RowSum rt = rows[0][lane % kJudge], rp = has_p ? rows[1][lane % kJudge] : RowSum{1.0, 0.f};
       const bool t_ok = is_distribution(rt);
       const int bad = !d_ok ? 1 : !t_ok || !is_distribution(rp) ? 2 : 0;
-      const double p = exp_neg<false>((double)zt - (double)rt.m) / rt.s;
-      const double q = has_p ? exp_neg<false>((double)zp - (double)rp.m) / rp.s : 1.0;
+      const double p = exp_neg((double)zt - (double)rt.m) / rt.s;
+      const double q = has_p ? exp_neg((double)zp - (double)rp.m) / rp.s : 1.0;
       const bool end = pos && (j == n || bad || !((double)u * q < p));
       const uint64_t ends = __ballot(end);
       if (!done && ends && lane == __builtin_ctzll(ends)) {
@@ -290,39 +283,22 @@ __device__ __forceinline__ void write_bad(const VerifyArgs& a, int s, const Verd
 
 // -------------------------------------------------------------- residual
 
-// What is left of words w0 .. w0 + 7 for the draw (of those below w0 + n).
-template <class TT, class TP>
-__device__ __forceinline__ void residual8(const VerifyArgs& a, const Verdict& v, int w0, int n, double (&r)[8]) {
+// What is left of words w0 .. w0 + 7 for the draw (nothing of those past V).
+__device__ __forceinline__ void residual8(const VerifyArgs& a, const Verdict& v, int w0, double (&r)[8]) {
   float xt[8], xp[8];
   const bool minus = v.p_row >= 0 && !v.whole;
-  load8((const TT*)a.target, v.t_row * a.ld_t + w0, n, xt);
+  load8(a.target, a.target16, v.t_row * a.ld_t + w0, a.V - w0, xt);
+  if (minus) load8(a.proposal, a.proposal16, v.p_row * a.ld_p + w0, a.V - w0, xp);
+  const double it = 1.0 / v.rt.s;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = exp_neg((double)xt[e] - (double)v.rt.m) * it;
   if (minus) {
-    load8((const TP*)a.proposal, v.p_row * a.ld_p + w0, n, xp);
-  } else {
+    const double ip = 1.0 / v.rp.s;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) xp[e] = -INFINITY;
-  }
-  const double it = 1.0 / v.rt.s, ip = minus ? 1.0 / v.rp.s : 0.0, mp = minus ? v.rp.m : 0.0;
+    for (int e = 0; e < 8; ++e) r[e] = fmax(r[e] - exp_neg((double)xp[e] - (double)v.rp.m) * ip, 0.0);
+  } else if (v.cut >= 0 && !v.whole) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    r[e] = exp_neg<true>((double)xt[e] - (double)v.rt.m) * it;
-    if (minus) r[e] -= exp_neg<true>((double)xp[e] - mp) * ip;
-    // (the bulk form's nothing is no probability)
-    if (r[e] < 1e-290 || (w0 + e == v.cut && !v.whole)) r[e] = 0.0;
-  }
-}
-__device__ __forceinline__ void residual8(const VerifyArgs& a, const Verdict& v, int w0, double (&r)[8]) {
-  const int n = a.V - w0;
-  if (a.target16) {
-    if (a.proposal16)
-      residual8<__bf16, __bf16>(a, v, w0, n, r);
-    else
-      residual8<__bf16, float>(a, v, w0, n, r);
-  } else {
-    if (a.proposal16)
-      residual8<float, __bf16>(a, v, w0, n, r);
-    else
-      residual8<float, float>(a, v, w0, n, r);
+    for (int e = 0; e < 8; ++e) r[e] = w0 + e == v.cut ? 0.0 : r[e];
   }
 }
 __device__ __forceinline__ double sum8(const double (&r)[8]) {
@@ -478,13 +454,13 @@ __global__ __launch_bounds__(2 * kJudge * 64) void k_verify_small(VerifyArgs a) 
   __shared__ Verdict shared_v;
   const int s = blockIdx.x, o0 = a.off[s], o1 = a.off[s + 1];
   judge(a, s, o0, o1, &shared_v, [&](bool tgt, int64_t row) {
+    const void* z = tgt ? a.target : a.proposal;
+    const int is16 = tgt ? a.target16 : a.proposal16;
+    const int64_t at = row * (tgt ? a.ld_t : a.ld_p);
     RowSum r{0.0, -INFINITY};
 #pragma unroll 1
     for (int i = 0; i < a.V; i += kPart) {
-      const int n = min(kPart, a.V - i);
-      const RowSum p = (tgt ? a.target16 : a.proposal16)
-                           ? part_sum((const __bf16*)(tgt ? a.target : a.proposal) + row * (tgt ? a.ld_t : a.ld_p) + i, n)
-                           : part_sum((const float*)(tgt ? a.target : a.proposal) + row * (tgt ? a.ld_t : a.ld_p) + i, n);
+      const RowSum p = part_sum(z, is16, at + i, min(kPart, a.V - i));
       r = i ? merge(r, p) : p;
     }
     return r;
