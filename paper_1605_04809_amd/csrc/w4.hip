@@ -9,9 +9,13 @@
 // blocks of a column tile after one another: 16-byte vector 16 q + r of a
 // tile belongs to column r, its 32-bit word s to rows 32 s + 8 q .. + 7 of the
 // block, nibble p of the word to row 2p (p < 4) or 2(p - 4) + 1.  Scales and
-// zero points are kept per tile, [tile][group][16].
+// zero points go with the tiles, [tile][row block][16][gpb]: gpb = 4, 2 or 1
+// for groups of whole 32s, 64s or 128s of rows (a group's scale stands once
+// for each of them), zeros past the last row.
+#include <algorithm>
 #include <cmath>
 #include <new>
+#include <type_traits>
 
 #include "draft.hpp"
 
@@ -22,7 +26,7 @@ constexpr int kW4Cols = 16, kW4Rows = 128;  // columns and rows of a packed tile
 struct nmt_w4 {
   nmt_w4_dims dims{};
   int device = 0, cus = 0;
-  int tiles = 0, kblocks = 0, groups = 0;
+  int tiles = 0, kblocks = 0, gpb = 1;
   void* mem = nullptr;  // everything below
   uint4* codes = nullptr;
   void* scales = nullptr;  // fp32 or bf16
@@ -59,21 +63,32 @@ __global__ __launch_bounds__(256) void k_w4_pack(const uint8_t* __restrict__ src
   out[i] = uint4{w[0], w[1], w[2], w[3]};
 }
 
+// Where entry i of the scales belongs: its column, and its first row.
+struct ScaleAt {
+  int64_t n;
+  int k;
+};
+__device__ __forceinline__ ScaleAt scale_at(int64_t i, int kblocks, int gpb) {
+  const int64_t tb = i / (kW4Cols * gpb);
+  return ScaleAt{tb / kblocks * kW4Cols + i / gpb % kW4Cols,
+                 (int)(tb % kblocks) * kW4Rows + (int)(i % gpb) * (kW4Rows / gpb)};
+}
+
 // Scales (fp32 to ST, nearest even), zero points and bias into their places;
-// zeros past the last column.
+// zeros past the last column and row.
 template <class ST>
 __global__ __launch_bounds__(256) void k_w4_params(const float* __restrict__ scales, const uint8_t* __restrict__ zeros,
-                                                   const float* __restrict__ bias, int N, int groups, int64_t n_all,
-                                                   ST* __restrict__ s_out, uint8_t* __restrict__ z_out,
-                                                   float* __restrict__ b_out) {
+                                                   const float* __restrict__ bias, int K, int N, int group, int kblocks,
+                                                   int gpb, int64_t n_all, ST* __restrict__ s_out,
+                                                   uint8_t* __restrict__ z_out, float* __restrict__ b_out) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n_all) return;
-  const int64_t tile = i / (kW4Cols * (int64_t)groups);
-  const int g = (int)(i / kW4Cols % groups);
-  const int64_t n = tile * kW4Cols + i % kW4Cols;
-  s_out[i] = (ST)(n < N ? scales[(int64_t)g * N + n] : 0.f);
-  if (zeros) z_out[i] = n < N ? zeros[(int64_t)g * N + n] : 0;
-  if (bias && g == 0) b_out[n] = n < N ? bias[n] : 0.f;
+  const ScaleAt at = scale_at(i, kblocks, gpb);
+  const bool in = at.n < N && at.k < K;
+  const int64_t from = in ? (int64_t)(at.k / group) * N + at.n : 0;
+  s_out[i] = (ST)(in ? scales[from] : 0.f);
+  if (zeros) z_out[i] = in ? zeros[from] : 0;
+  if (bias && at.k == 0) b_out[at.n] = at.n < N ? bias[at.n] : 0.f;
 }
 
 // A model's output weight (k, n) from its packed matrix.
@@ -82,34 +97,30 @@ __device__ __forceinline__ float out_weight(const void* W, bool bf16, int64_t Np
               : ((const float*)W)[((int64_t)(k / 4) * Npad + n) * 4 + k % 4];
 }
 
-// Scales of the model's columns, one thread per (tile, group, column): the
-// group's largest magnitude / 7.
+// Scales of the model's columns, one thread an entry: the group's largest
+// magnitude / 7.
 template <class ST>
 __global__ __launch_bounds__(256) void k_w4_out_scales(const void* __restrict__ W, int bf16, int64_t Npad, int K, int N,
-                                                       int group, int groups, int krow, int nbias, int64_t n_all,
-                                                       ST* __restrict__ s_out, float* __restrict__ b_out,
+                                                       int group, int kblocks, int gpb, int krow, int nbias,
+                                                       int64_t n_all, ST* __restrict__ s_out, float* __restrict__ b_out,
                                                        int* __restrict__ bad) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n_all) return;
-  const int64_t tile = i / (kW4Cols * (int64_t)groups);
-  const int g = (int)(i / kW4Cols % groups);
-  const int64_t n = tile * kW4Cols + i % kW4Cols;
+  const ScaleAt at = scale_at(i, kblocks, gpb);
   float mx = 0.f;
   bool finite = true;
-  if (n < N) {
-    const int k1 = min(K, (g + 1) * group);
-    for (int k = g * group; k < k1; ++k) {
-      const float a = fabsf(out_weight(W, bf16, Npad, k, n));
+  if (at.n < N) {
+    const int k0 = at.k / group * group, k1 = at.k < K ? min(K, k0 + group) : 0;
+    for (int k = k0; k < k1; ++k) {
+      const float a = fabsf(out_weight(W, bf16, Npad, k, at.n));
       finite = finite && a < INFINITY;
       mx = fmaxf(mx, a);
     }
-    if (g == 0) {
-      float b = 0.f;
-      for (int j = 0; j < nbias; ++j) b += out_weight(W, bf16, Npad, krow + j, n);
-      b_out[n] = b;
-    }
-  } else if (g == 0) {
-    b_out[n] = 0.f;
+  }
+  if (at.k == 0) {
+    float b = 0.f;
+    for (int j = 0; j < nbias && at.n < N; ++j) b += out_weight(W, bf16, Npad, krow + j, at.n);
+    b_out[at.n] = b;
   }
   s_out[i] = (ST)(mx / 7.f);
   // (a scale that rounds up to infinity is as useless as an infinite weight)
@@ -119,7 +130,7 @@ __global__ __launch_bounds__(256) void k_w4_out_scales(const void* __restrict__ 
 // The codes under those scales, one packed vector per thread.
 template <class ST>
 __global__ __launch_bounds__(256) void k_w4_out_codes(const void* __restrict__ W, int bf16, int64_t Npad, int K, int N,
-                                                      int group, int groups, int kblocks, int64_t n_all,
+                                                      int kblocks, int gpb, int64_t n_all,
                                                       const ST* __restrict__ scales, uint4* __restrict__ out) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n_all) return;
@@ -136,7 +147,7 @@ __global__ __launch_bounds__(256) void k_w4_out_codes(const void* __restrict__ W
       const int k = kb * kW4Rows + s * 32 + q * 8 + nibble_row(p);
       uint32_t c = 8;
       if (k < K && n < N) {
-        const float sc = (float)scales[(tile * groups + k / group) * kW4Cols + r];
+        const float sc = (float)scales[(tb * kW4Cols + r) * gpb + s * gpb / 4];
         const float v = sc != 0.f ? rintf(out_weight(W, bf16, Npad, k, n) / sc) : 0.f;
         c = (uint32_t)(8 + (int)fminf(fmaxf(v, -7.f), 7.f));
       }
@@ -147,56 +158,336 @@ __global__ __launch_bounds__(256) void k_w4_out_codes(const void* __restrict__ W
 }
 
 // ------------------------------------------------------------- product
+//
+// On the fp16 matrix cores: codes minus their zero point are whole numbers of
+// at most 15, exact in fp16, and the inputs enter as fp16 times a power of two,
+// an fp32 input as two halves hi = fp16(x 2^e) and lo = fp16(x 2^e - hi), 22
+// bits and a sign, a bf16 input as one.  e puts the row's largest input in
+// [2^14, 2^15), so an input is off by at most 2^-24 of itself or 2^-40 of that
+// largest one.  A group's products are summed in fp32 by the MFMA, then times
+// the scale to the row's sum.
+//
+// A block of 8 waves covers WN = 8 / WK groups of NT column tiles and up to
+// 16 RT rows.  It finds its rows' largest inputs, then takes them to LDS as
+// MFMA fragments, a chunk of K at a time, converted once a block; the codes
+// stream from memory straight into registers, two K blocks ahead, each 16-byte
+// vector the operand of four MFMA steps of 32 rows of W: 9 instructions turn a
+// 32-bit word into eight fp16 values (0x6400 | n is 1024 + n; the upper nibble
+// of a byte, in place, gives 1024 + 16 n).  Lane 16 q + r holds column r, so a
+// lane needs one scale and one zero point a group.  WK > 1 splits K between
+// waves where there are few columns; their sums meet in LDS at the end, in a
+// fixed order.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kW4Threads = 512, kW4Waves = 8;
+constexpr int kStageVectors = 2048;  // 8-element vectors of a chunk: rows x 16 a K block
+constexpr int kW4MaxRows = 64;
 
 struct W4Args {
   const uint4* codes;
   const void* scales;
   const uint8_t* zeros;
   const float* bias;
-  int K, N, group, groups, kblocks, M;
+  int K, N, kblocks, tiles, M;
+  int y16;
   const void* x;
   int64_t ld_x;
   void* y;
   int64_t ld_y;
 };
+// How a launch is cut: rows a block (at most 16 RT), row blocks, waves that
+// share a column group's K, K blocks a chunk (a multiple of 2 wk, or all).
+struct W4Shape {
+  int rows, row_blocks, wk, chunk;
+};
 
-// One output a thread: 16 columns of a tile times 16 rows of x in a block.
-template <class XT, class YT, class ST>
-__global__ __launch_bounds__(256) void k_w4_product(W4Args a) {
-  const int r = threadIdx.x & 15;
-  const int64_t tile = blockIdx.x, n = tile * kW4Cols + r, m = (int64_t)blockIdx.y * 16 + (threadIdx.x >> 4);
-  if (n >= a.N || m >= a.M) return;
-  const XT* x = (const XT*)a.x + m * a.ld_x;
-  float sum = 0.f, part = 0.f;
-  for (int k0 = 0; k0 < a.K; k0 += 8) {
-    const int s = k0 / 32 % 4, q = k0 / 8 % 4, g = k0 / a.group;
-    const uint32_t w = ((const uint32_t*)(a.codes + (tile * a.kblocks + k0 / kW4Rows) * 64 + q * 16 + r))[s];
-    const float z = a.zeros ? (float)a.zeros[(tile * a.groups + g) * kW4Cols + r] : 8.f;
-    for (int p = 0; p < 8; ++p) {
-      const int k = k0 + nibble_row(p);
-      if (k < a.K) part = fmaf((float)x[k], (float)((w >> (4 * p)) & 15u) - z, part);
-    }
-    if ((k0 + 8) % a.group == 0 || k0 + 8 >= a.K) {
-      sum = fmaf(part, (float)((const ST*)a.scales)[(tile * a.groups + g) * kW4Cols + r], sum);
-      part = 0.f;
-    }
+// Eight consecutive elements of a row, those from n on as zeros; any alignment
+// of the elements' own.
+typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
+__device__ __forceinline__ void load8(const float* x, int n, float (&v)[8]) {
+  if (n >= 8) {
+    const f32x4u a = *(const f32x4u*)x, b = *(const f32x4u*)(x + 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < 4 ? a[e] : b[e - 4];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? x[e] : 0.f;
   }
-  if (a.bias) sum += a.bias[n];
-  ((YT*)a.y)[m * a.ld_y + n] = (YT)sum;
+}
+__device__ __forceinline__ void load8(const __bf16* x, int n, float (&v)[8]) {
+  if (n >= 8) {
+    const bf16x8u a = *(const bf16x8u*)x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)a[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? (float)x[e] : 0.f;
+  }
 }
 
-template <class XT, class YT, class ST>
-hipError_t launch_product(const W4Args& a, int tiles, hipStream_t st) {
-  for (int m0 = 0; m0 < a.M; m0 += 16 * 65535) {  // rows per launch: the grid's limit
-    W4Args b = a;
-    b.M = a.M - m0 < 16 * 65535 ? a.M - m0 : 16 * 65535;
-    b.x = (const XT*)a.x + (int64_t)m0 * a.ld_x;
-    b.y = (YT*)a.y + (int64_t)m0 * a.ld_y;
-    hipLaunchKernelGGL((k_w4_product<XT, YT, ST>), dim3(tiles, ceil_div(b.M, 16)), dim3(256), 0, st, b);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+// Eight codes of a word as fp16, minus the zero point: zl = -(1024 + z) and
+// zh = -(64 + z), twice each.  (The masks sit in scalar registers, or the
+// compiler splits each and-or for the sake of its literals.)
+struct Masks {
+  uint32_t lo = 0x000f000fu, hi = 0x00f000f0u, base = 0x64006400u;
+  __device__ __forceinline__ Masks() { asm("" : "+s"(lo), "+s"(hi), "+v"(base)); }
+};
+__device__ __forceinline__ f16x8 codes_f16(uint32_t w, f16x2 zl, f16x2 zh, const Masks& k) {
+  const f16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
+  auto h2 = [](uint32_t u) { return __builtin_bit_cast(f16x2, u); };
+  const uint32_t w8 = w >> 8;
+  const f16x2 a = h2((w & k.lo) | k.base) + zl;
+  const f16x2 b = __builtin_elementwise_fma(h2((w & k.hi) | k.base), sixteenth, zh);
+  const f16x2 c = h2((w8 & k.lo) | k.base) + zl;
+  const f16x2 d = __builtin_elementwise_fma(h2((w8 & k.hi) | k.base), sixteenth, zh);
+  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The largest of 16 consecutive lanes' values, in all of them.
+__device__ __forceinline__ float max16(float v) {
+  auto with = [&](auto ctrl) {
+    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf,
+                                                                    0xf, true)));
+  };
+  with(std::integral_constant<int, 0xB1>{});   // lane ^ 1
+  with(std::integral_constant<int, 0x4E>{});   // lane ^ 2
+  with(std::integral_constant<int, 0x141>{});  // 7 - lane of 8
+  with(std::integral_constant<int, 0x140>{});  // 15 - lane of 16
+  return v;
+}
+
+template <int RT, int NT, int GPB, bool X16, bool S16>
+__global__ __launch_bounds__(kW4Threads) __attribute__((amdgpu_waves_per_eu(RT == 4 ? 2 : 4))) void k_w4_product(
+    W4Args a, W4Shape sh) {
+  constexpr int HV = X16 ? 1 : 2;  // fp16 parts of an input
+  using XT = std::conditional_t<X16, __bf16, float>;
+  using ST = std::conditional_t<S16, __bf16, float>;
+  extern __shared__ f32x4 lds[];   // [K block][step][part][lane quarter][row]
+  __shared__ uint32_t row_max[kW4MaxRows];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, q = lane >> 4;
+  // the row blocks of the same columns run on one XCD, whose L2 then holds their codes
+  const int id = blockIdx.x, slot = id >> 3;
+  const int cb = (slot / sh.row_blocks) * 8 + (id & 7), rb = slot % sh.row_blocks;
+  const int wn = kW4Waves / sh.wk, wk = wave % sh.wk;
+  const int tile0 = (cb * wn + wave / sh.wk) * NT;
+  if (cb * wn * NT >= a.tiles) return;
+  const int row0 = rb * sh.rows, rows = min(sh.rows, a.M - row0);
+
+  // a K block's codes, scales and zero points for this wave (past the end: some that exist), as they are in memory
+  typedef ST scales_t __attribute__((ext_vector_type(GPB)));
+  struct Block {
+    uint4 code[NT];
+    scales_t scale[NT];
+    uint32_t zero[NT];
+  };
+  auto load = [&](Block& b, int kb) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int64_t tb = (int64_t)min(tile0 + t, a.tiles - 1) * a.kblocks + min(kb, a.kblocks - 1);
+      b.code[t] = (a.codes + tb * 64)[lane];
+      b.scale[t] = ((const scales_t*)a.scales + tb * kW4Cols)[r16];
+      b.zero[t] = 0x08080808u;
+      if (a.zeros) {
+        if constexpr (GPB == 4)
+          b.zero[t] = ((const uint32_t*)a.zeros + tb * kW4Cols)[r16];
+        else if constexpr (GPB == 2)
+          b.zero[t] = ((const uint16_t*)a.zeros + tb * kW4Cols)[r16];
+        else
+          b.zero[t] = (a.zeros + tb * kW4Cols)[r16];
+      }
+    }
+  };
+  const Masks masks;
+  Block b0, b1;
+  load(b0, wk);
+  load(b1, wk + sh.wk);
+
+  // the rows' largest inputs
+  if (tid < kW4MaxRows) row_max[tid] = 0;
+  __syncthreads();
+  const XT* x = (const XT*)a.x + (int64_t)row0 * a.ld_x;
+  // (16 lanes take a K block of a row)
+  auto each_vector = [&](int nkb, auto&& f) {  // f(row, vector of the row)
+    const int dk = kW4Threads / 16 % nkb, dm = kW4Threads / 16 / nkb;
+    int kb = (tid >> 4) % nkb;
+    for (int m = (tid >> 4) / nkb; m < rows; m += dm) {
+      f(m, kb * 16 + r16);
+      kb += dk;
+      if (kb >= nkb) {
+        kb -= nkb;
+        ++m;
+      }
+    }
+  };
+  each_vector(a.kblocks, [&](int m, int kv) {
+    float v[8], mx = 0.f;
+    load8(x + m * a.ld_x + kv * 8, a.K - kv * 8, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float f = fabsf(v[e]);
+      mx = f < INFINITY ? fmaxf(mx, f) : mx;
+    }
+    mx = max16(mx);
+    if (r16 == 0) atomicMax(&row_max[m], __builtin_bit_cast(uint32_t, mx));
+  });
+  __syncthreads();
+  // the power of two that puts a row's largest in [2^14, 2^15); not above 2^120, whose reciprocal is normal
+  auto exponent = [&](int m) {
+    const float mx = __builtin_bit_cast(float, row_max[m]);
+    return mx > 0.f ? min(15 - __builtin_amdgcn_frexp_expf(mx), 120) : 0;
+  };
+
+  f32x4 sum[NT][RT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < RT; ++i) sum[t][i] = zero4();
+  for (int kb0 = 0; kb0 < a.kblocks; kb0 += sh.chunk) {
+    const int nkb = min(sh.chunk, a.kblocks - kb0);
+    if (kb0 > 0) __syncthreads();
+    each_vector(nkb, [&](int m, int kv) {
+      const int k = kb0 * kW4Rows + kv * 8, e2 = exponent(m);
+      float v[8];
+      load8(x + m * a.ld_x + k, a.K - k, v);
+      f16x8 hi, lo;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float f = __builtin_amdgcn_ldexpf(v[e], e2);
+        hi[e] = (_Float16)f;
+        // (an infinity or NaN is all in hi)
+        lo[e] = fabsf(f) < INFINITY ? (_Float16)(f - (float)hi[e]) : (_Float16)0.f;
+      }
+      f32x4* to = lds + ((kv >> 2) * HV * 4 + (kv & 3)) * rows + m;
+      to[0] = __builtin_bit_cast(f32x4, hi);
+      if constexpr (HV == 2) to[4 * rows] = __builtin_bit_cast(f32x4, lo);
+    });
+    __syncthreads();
+
+    auto compute = [&](const Block& b, int kl) {
+      const f32x4* from = lds + (kl * 16 * HV + q) * rows;
+      f32x4 acc[NT][RT];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        constexpr int kStepsPerGroup = 4 / GPB;
+        const bool first = s % kStepsPerGroup == 0;
+        const int g = s / kStepsPerGroup;
+        f32x4 xf[RT][HV];
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int z = 0; z < HV; ++z) xf[i][z] = from[(s * HV + z) * 4 * rows + min(i * 16 + r16, rows - 1)];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          // the group's zero point in both halves; -(1024 + z) and -(64 + z) as bits
+          const uint32_t z = __builtin_amdgcn_perm(0u, b.zero[t], 0x0c000c00u | (uint32_t)g * 0x00010001u);
+          const f16x2 zl = __builtin_bit_cast(f16x2, z | 0xe400e400u);
+          const f16x2 zh = __builtin_bit_cast(f16x2, (z << 4) | 0xd400d400u);
+          const uint32_t w = s == 0 ? b.code[t].x : s == 1 ? b.code[t].y : s == 2 ? b.code[t].z : b.code[t].w;
+          const f16x8 c = codes_f16(w, zl, zh, masks);
+#pragma unroll
+          for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int h = HV - 1; h >= 0; --h)
+              acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, xf[i][h]), c,
+                                                                 first && h == HV - 1 ? zero4() : acc[t][i], 0, 0, 0);
+        }
+        if ((s + 1) % kStepsPerGroup == 0)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sum[t][i][e] = fmaf(acc[t][i][e], (float)b.scale[t][g], sum[t][i][e]);
+      }
+    };
+    for (int kl = wk; kl < nkb; kl += 2 * sh.wk) {
+      compute(b0, kl);
+      load(b0, kb0 + kl + 2 * sh.wk);
+      if (kl + sh.wk >= nkb) break;
+      compute(b1, kl + sh.wk);
+      load(b1, kb0 + kl + 3 * sh.wk);
+    }
   }
-  return hipSuccess;
+
+  if (sh.wk > 1) {  // the K shares' sums, in order
+    __syncthreads();
+    f32x4* red = lds + (wave * NT * RT) * 64 + lane;
+    if (wk > 0)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) red[(t * RT + i) * 64] = sum[t][i];
+    __syncthreads();
+    if (wk > 0) return;
+    for (int w = 1; w < sh.wk; ++w)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) sum[t][i] += red[(w * NT * RT + t * RT + i) * 64];
+  }
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int m = i * 16 + 4 * q + e;
+      if (m >= rows) continue;
+      const float unit = __builtin_amdgcn_ldexpf(1.f, -exponent(m));
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int64_t n = (int64_t)(tile0 + t) * kW4Cols + r16, at = (int64_t)(row0 + m) * a.ld_y + n;
+        if (n >= a.N) continue;
+        const float y = fmaf(sum[t][i][e], unit, a.bias ? a.bias[n] : 0.f);
+        if (a.y16)
+          ((__bf16*)a.y)[at] = (__bf16)y;
+        else
+          ((float*)a.y)[at] = y;
+      }
+    }
+}
+
+template <int RT, int NT, int GPB, bool X16, bool S16>
+hipError_t launch_form(const W4Args& a, const W4Shape& sh, hipStream_t st) {
+  const int wn = kW4Waves / sh.wk;
+  const int64_t cbs = round_up(ceil_div(a.tiles, wn * NT), 8), grid = cbs * sh.row_blocks;
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  // a chunk's fragments, or the K shares' sums
+  const size_t frag = (size_t)std::min(sh.rows, a.M) * sh.chunk * 16 * (X16 ? 16 : 32);
+  const size_t red = sh.wk > 1 ? (size_t)kW4Waves * NT * RT * 64 * 16 : 0;
+  hipLaunchKernelGGL((k_w4_product<RT, NT, GPB, X16, S16>), dim3((unsigned)grid), dim3(kW4Threads), std::max(frag, red),
+                     st, a, sh);
+  return hipGetLastError();
+}
+
+hipError_t launch_product(const W4Args& a, bool x16, bool s16, int gpb, int cus, hipStream_t st) {
+  // rows evenly over blocks of at most 64
+  W4Shape sh{};
+  sh.row_blocks = ceil_div(a.M, kW4MaxRows);
+  const int rt16 = ceil_div(ceil_div(a.M, sh.row_blocks), 16), RT = rt16 > 2 ? 4 : rt16;
+  sh.rows = a.M < 16 ? a.M : rt16 * 16;
+  // K blocks of the largest chunk; K split between waves while there are fewer than about 8 waves a CU
+  const int most = std::min(kStageVectors / 16 / sh.rows, a.kblocks);
+  const int NT = RT == 1 && a.tiles < 4 * cus ? 1 : 2;
+  sh.wk = 1;
+  while (sh.wk < kW4Waves && (sh.wk * 4 <= most || (most == a.kblocks && sh.wk * 2 <= most)) &&
+         (int64_t)ceil_div(a.tiles, NT) * sh.row_blocks * sh.wk < 8 * cus)
+    sh.wk *= 2;
+  sh.chunk = most == a.kblocks ? most : most / (2 * sh.wk) * (2 * sh.wk);
+  auto types = [&](auto rt, auto nt, auto g) {
+    constexpr int R = decltype(rt)::value, T = decltype(nt)::value, G = decltype(g)::value;
+    return x16 ? (s16 ? launch_form<R, T, G, true, true>(a, sh, st) : launch_form<R, T, G, true, false>(a, sh, st))
+               : (s16 ? launch_form<R, T, G, false, true>(a, sh, st) : launch_form<R, T, G, false, false>(a, sh, st));
+  };
+  auto groups = [&](auto rt, auto nt) {
+    return gpb == 4   ? types(rt, nt, std::integral_constant<int, 4>{})
+           : gpb == 2 ? types(rt, nt, std::integral_constant<int, 2>{})
+                      : types(rt, nt, std::integral_constant<int, 1>{});
+  };
+  constexpr std::integral_constant<int, 1> I1{};
+  constexpr std::integral_constant<int, 2> I2{};
+  constexpr std::integral_constant<int, 4> I4{};
+  return RT == 1 ? (NT == 1 ? groups(I1, I1) : groups(I1, I2)) : RT == 2 ? groups(I2, I2) : groups(I4, I2);
 }
 
 bool known_type(int32_t t) { return t == NMT_F32 || t == NMT_BF16; }
@@ -212,7 +503,7 @@ nmt_status w4_new(const nmt_w4_dims& d, bool zeros, bool bias, nmt_w4** out) {
   w->dims = d;
   w->tiles = ceil_div(d.N, kW4Cols);
   w->kblocks = ceil_div(d.K, kW4Rows);
-  w->groups = ceil_div(d.K, d.group);
+  w->gpb = d.group % 128 == 0 ? 1 : d.group % 64 == 0 ? 2 : 4;
   hipError_t e = hipGetDevice(&w->device);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&w->cus, hipDeviceAttributeMultiprocessorCount, w->device);
   size_t bytes = 0;
@@ -221,7 +512,7 @@ nmt_status w4_new(const nmt_w4_dims& d, bool zeros, bool bias, nmt_w4** out) {
     bytes += (n + 255) / 256 * 256;
     return o;
   };
-  const size_t nsc = (size_t)w->tiles * w->groups * kW4Cols;
+  const size_t nsc = (size_t)w->tiles * w->kblocks * kW4Cols * w->gpb;
   const size_t o_codes = part((size_t)w->tiles * w->kblocks * 1024), o_sc = part(nsc * (d.stype == NMT_BF16 ? 2 : 4)),
                o_z = part(zeros ? nsc : 0), o_b = part(bias ? (size_t)w->tiles * kW4Cols * 4 : 0);
   if (e == hipSuccess) e = device_malloc(&w->mem, bytes);
@@ -272,14 +563,14 @@ nmt_status nmt_w4_create(const nmt_w4_dims* dims, const uint8_t* h_codes, const 
   if (e == hipSuccess && h_zeros) e = hipMemcpy(raw + o_z, h_zeros, ng, hipMemcpyHostToDevice);
   if (e == hipSuccess && h_bias) e = hipMemcpy(raw + o_b, h_bias, (size_t)d.N * 4, hipMemcpyHostToDevice);
   if (e == hipSuccess) {
-    const int64_t nv = (int64_t)w->tiles * w->kblocks * 64, np = (int64_t)w->tiles * w->groups * kW4Cols;
+    const int64_t nv = (int64_t)w->tiles * w->kblocks * 64, np = (int64_t)w->tiles * w->kblocks * kW4Cols * w->gpb;
     hipLaunchKernelGGL(k_w4_pack, dim3((unsigned)((nv + 255) / 256)), dim3(256), 0, nullptr, (const uint8_t*)raw, d.K,
                        d.N, w->kblocks, nv, w->codes);
     auto params = [&](auto* s_out) {
       hipLaunchKernelGGL((k_w4_params<std::remove_pointer_t<decltype(s_out)>>), dim3((unsigned)((np + 255) / 256)),
                          dim3(256), 0, nullptr, (const float*)(raw + o_s),
                          h_zeros ? (const uint8_t*)(raw + o_z) : nullptr, h_bias ? (const float*)(raw + o_b) : nullptr,
-                         d.N, w->groups, np, s_out, w->zeros, w->bias);
+                         d.K, d.N, d.group, w->kblocks, w->gpb, np, s_out, w->zeros, w->bias);
     };
     if (d.stype == NMT_BF16)
       params((__bf16*)w->scales);
@@ -309,7 +600,7 @@ nmt_status nmt_w4_from_output(const nmt_model* m, int32_t group, int32_t stype, 
   if (rc != NMT_OK) return rc;
   hipStream_t st = (hipStream_t)stream;
   const Packed& P = *o.W;
-  const int64_t nv = (int64_t)w->tiles * w->kblocks * 64, np = (int64_t)w->tiles * w->groups * kW4Cols;
+  const int64_t nv = (int64_t)w->tiles * w->kblocks * 64, np = (int64_t)w->tiles * w->kblocks * kW4Cols * w->gpb;
   int* bad = nullptr;
   int h_bad = 0;
   hipError_t e = device_malloc((void**)&bad, sizeof(int));
@@ -317,9 +608,9 @@ nmt_status nmt_w4_from_output(const nmt_model* m, int32_t group, int32_t stype, 
   auto quantise = [&](auto* sc) {
     using ST = std::remove_pointer_t<decltype(sc)>;
     hipLaunchKernelGGL((k_w4_out_scales<ST>), dim3((unsigned)((np + 255) / 256)), dim3(256), 0, st, P.d, (int)P.bf16,
-                       P.Npad, o.E, o.V, group, w->groups, P.Krows, P.nbias, np, sc, w->bias, bad);
+                       P.Npad, o.E, o.V, group, w->kblocks, w->gpb, P.Krows, P.nbias, np, sc, w->bias, bad);
     hipLaunchKernelGGL((k_w4_out_codes<ST>), dim3((unsigned)((nv + 255) / 256)), dim3(256), 0, st, P.d, (int)P.bf16,
-                       P.Npad, o.E, o.V, group, w->groups, w->kblocks, nv, (const ST*)sc, w->codes);
+                       P.Npad, o.E, o.V, w->kblocks, w->gpb, nv, (const ST*)sc, w->codes);
   };
   if (e == hipSuccess) {
     if (stype == NMT_BF16)
@@ -357,21 +648,15 @@ nmt_status nmt_w4_product(const nmt_w4* w, int32_t M, const void* d_x, int32_t x
   if (M == 0) return entry_ok();
   if (!d_x || !d_y) return entry_fail(NMT_EINVAL, "a required device pointer is NULL");
   if (ld_x < w->dims.K || ld_y < w->dims.N) return entry_fail(NMT_EINVAL, "a row stride is below the row's length");
-  const bool x16 = x_type == NMT_BF16, y16 = y_type == NMT_BF16, s16 = w->dims.stype == NMT_BF16;
+  const bool x16 = x_type == NMT_BF16, y16 = y_type == NMT_BF16;
   if (((uintptr_t)d_x & (x16 ? 1 : 3)) || ((uintptr_t)d_y & (y16 ? 1 : 3)))
     return entry_fail(NMT_EINVAL, "d_x and d_y must be aligned to their elements");
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess) return entry_fail(NMT_EDEVICE, "hipGetDevice failed");
   if (dev != w->device) return entry_fail(NMT_EINVAL, "the 4-bit matrix lives on another device than the current one");
-  const W4Args a{w->codes, w->scales, w->zeros, w->bias, w->dims.K, w->dims.N, w->dims.group, w->groups, w->kblocks, M,
-                 d_x, ld_x, d_y, ld_y};
-  hipStream_t st = (hipStream_t)stream;
-  auto scales = [&](auto xt, auto yt) {
-    return s16 ? launch_product<decltype(xt), decltype(yt), __bf16>(a, w->tiles, st)
-               : launch_product<decltype(xt), decltype(yt), float>(a, w->tiles, st);
-  };
-  const hipError_t e = x16 ? (y16 ? scales(__bf16{}, __bf16{}) : scales(__bf16{}, float{}))
-                           : (y16 ? scales(float{}, __bf16{}) : scales(float{}, float{}));
+  const W4Args a{w->codes, w->scales, w->zeros, w->bias, w->dims.K, w->dims.N, w->kblocks, w->tiles, M, y16,
+                 d_x,      ld_x,      d_y,      ld_y};
+  const hipError_t e = launch_product(a, x16, w->dims.stype == NMT_BF16, w->gpb, w->cus, (hipStream_t)stream);
   if (e != hipSuccess) return entry_hip_fail(e, "nmt_w4_product");
   return entry_ok();
 }
