@@ -248,9 +248,11 @@ def _checked(t, dtype, n: int, what: str):
 
 
 def _stream(stream) -> Optional[int]:
+    if stream is not None:
+        return stream.cuda_stream
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    # the current stream's handle without a Stream object around it (2.6 us a call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 class Model:
