@@ -162,27 +162,25 @@ __global__ __launch_bounds__(256) void k_w4_out_codes(const void* __restrict__ W
 // On the fp16 matrix cores: codes minus their zero point are whole numbers of
 // at most 15, exact in fp16, and the inputs enter as fp16 times a power of two,
 // an fp32 input as two halves hi = fp16(x 2^e) and lo = fp16(x 2^e - hi), 22
-// bits and a sign, a bf16 input as one.  e puts the row's largest input in
-// [2^14, 2^15), so an input is off by at most 2^-24 of itself or 2^-40 of that
-// largest one.  A group's products are summed in fp32 by the MFMA, then times
-// the scale to the row's sum.
+// bits and a sign, a bf16 input as one.  e puts the largest of a row's 128
+// inputs of a K block in [2^14, 2^15), so an input is off by at most 2^-24 of
+// itself or 2^-40 of that largest one.  A group's products are summed in fp32
+// by the MFMA, then times the scale to the block's sum and times 2^-e to the
+// row's.
 //
-// A block of 8 waves covers WN = 8 / WK groups of NT column tiles and up to
-// 16 RT rows.  It finds its rows' largest inputs, then takes them to LDS as
-// MFMA fragments, a chunk of K at a time, converted once a block; the codes
-// stream from memory straight into registers, two K blocks ahead, each 16-byte
-// vector the operand of four MFMA steps of 32 rows of W: 9 instructions turn a
-// 32-bit word into eight fp16 values (0x6400 | n is 1024 + n; the upper nibble
-// of a byte, in place, gives 1024 + 16 n).  Lane 16 q + r holds column r, so a
-// lane needs one scale and one zero point a group.  WK > 1 splits K between
-// waves where there are few columns; their sums meet in LDS at the end, in a
-// fixed order.
+// A block of 8 waves takes up to RM rows and 8 NT / WK column tiles.  It holds
+// the rows' inputs in LDS as MFMA fragments, converted once a block (K too long
+// for LDS is taken in chunks).  The codes stream from memory straight into
+// registers, D K blocks ahead and from before the inputs are converted, each 16-byte vector the operand of four MFMA steps
+// of 32 rows of W: 9 instructions turn a 32-bit word into eight fp16 values
+// (0x6400 | n is 1024 + n; the upper nibble of a byte, in place, gives
+// 1024 + 16 n).  Lane 16 q + r holds column r of a tile, so it needs one scale
+// and one zero point a group.  WK > 1 splits K between waves where there are
+// few columns; their sums meet in LDS in a fixed order.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kW4Threads = 512, kW4Waves = 8;
-constexpr int kStageVectors = 2048;  // 8-element vectors of a chunk: rows x 16 a K block
-constexpr int kW4MaxRows = 64;
+constexpr int kW4Waves = 8;
 
 struct W4Args {
   const uint4* codes;
@@ -196,14 +194,33 @@ struct W4Args {
   void* y;
   int64_t ld_y;
 };
-// How a launch is cut: rows a block (at most 16 RT), row blocks, waves that
-// share a column group's K, K blocks a chunk (a multiple of 2 wk, or all).
+// How a launch is cut: rows a block (at most RM), row blocks, waves that share
+// a column's K, K blocks a chunk (a multiple of D wk, or all).
 struct W4Shape {
   int rows, row_blocks, wk, chunk;
 };
+constexpr int w4_depth(int RM) { return RM <= 16 ? 4 : 2; }  // K blocks in flight
 
-// Eight consecutive elements of a row, those from n on as zeros; any alignment
-// of the elements' own.
+// Eight codes of a word as fp16, minus the zero point: zl = -(1024 + z) and
+// zh = -(64 + z), twice each.  (The masks sit in registers, or the compiler
+// splits each and-or for the sake of its literals.)
+struct Masks {
+  uint32_t lo = 0x000f000fu, hi = 0x00f000f0u, base = 0x64006400u;
+  __device__ __forceinline__ Masks() { asm("" : "+s"(lo), "+s"(hi), "+v"(base)); }
+};
+__device__ __forceinline__ f16x8 codes_f16(uint32_t w, f16x2 zl, f16x2 zh, const Masks& k) {
+  const f16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
+  auto h2 = [](uint32_t u) { return __builtin_bit_cast(f16x2, u); };
+  const uint32_t w8 = w >> 8;
+  const f16x2 a = h2((w & k.lo) | k.base) + zl;
+  const f16x2 b = __builtin_elementwise_fma(h2((w & k.hi) | k.base), sixteenth, zh);
+  const f16x2 c = h2((w8 & k.lo) | k.base) + zl;
+  const f16x2 d = __builtin_elementwise_fma(h2((w8 & k.hi) | k.base), sixteenth, zh);
+  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Eight consecutive inputs, those from n on as zeros; any alignment of the
+// elements' own.
 typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
 __device__ __forceinline__ void load8(const float* x, int n, float (&v)[8]) {
   if (n >= 8) {
@@ -226,24 +243,6 @@ __device__ __forceinline__ void load8(const __bf16* x, int n, float (&v)[8]) {
   }
 }
 
-// Eight codes of a word as fp16, minus the zero point: zl = -(1024 + z) and
-// zh = -(64 + z), twice each.  (The masks sit in scalar registers, or the
-// compiler splits each and-or for the sake of its literals.)
-struct Masks {
-  uint32_t lo = 0x000f000fu, hi = 0x00f000f0u, base = 0x64006400u;
-  __device__ __forceinline__ Masks() { asm("" : "+s"(lo), "+s"(hi), "+v"(base)); }
-};
-__device__ __forceinline__ f16x8 codes_f16(uint32_t w, f16x2 zl, f16x2 zh, const Masks& k) {
-  const f16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
-  auto h2 = [](uint32_t u) { return __builtin_bit_cast(f16x2, u); };
-  const uint32_t w8 = w >> 8;
-  const f16x2 a = h2((w & k.lo) | k.base) + zl;
-  const f16x2 b = __builtin_elementwise_fma(h2((w & k.hi) | k.base), sixteenth, zh);
-  const f16x2 c = h2((w8 & k.lo) | k.base) + zl;
-  const f16x2 d = __builtin_elementwise_fma(h2((w8 & k.hi) | k.base), sixteenth, zh);
-  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
 // The largest of 16 consecutive lanes' values, in all of them.
 __device__ __forceinline__ float max16(float v) {
   auto with = [&](auto ctrl) {
@@ -257,25 +256,28 @@ __device__ __forceinline__ float max16(float v) {
   return v;
 }
 
-template <int RT, int NT, int GPB, bool X16, bool S16>
-__global__ __launch_bounds__(kW4Threads) __attribute__((amdgpu_waves_per_eu(RT == 4 ? 2 : 4))) void k_w4_product(
+template <int RM, int NT, int GPB, bool X16, bool S16>
+__global__ __launch_bounds__(kW4Waves * 64) __attribute__((amdgpu_waves_per_eu(RM > 32 ? 2 : 4))) void k_w4_product(
     W4Args a, W4Shape sh) {
+  constexpr int RT = (RM + 15) / 16, RS = RM + 1;  // row tiles; rows of an LDS fragment (odd, a constant: its steps
+                                                   // are offsets within the instructions)
   constexpr int HV = X16 ? 1 : 2;  // fp16 parts of an input
+  constexpr int D = w4_depth(RM);
   using XT = std::conditional_t<X16, __bf16, float>;
   using ST = std::conditional_t<S16, __bf16, float>;
-  extern __shared__ f32x4 lds[];   // [K block][step][part][lane quarter][row]
-  __shared__ uint32_t row_max[kW4MaxRows];
+  // [K block][step][part][lane quarter][row] fragments, then
+  // [K block][16 RT] 2^-e, then the K shares' sums
+  extern __shared__ f32x4 lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, q = lane >> 4;
   // the row blocks of the same columns run on one XCD, whose L2 then holds their codes
   const int id = blockIdx.x, slot = id >> 3;
   const int cb = (slot / sh.row_blocks) * 8 + (id & 7), rb = slot % sh.row_blocks;
-  const int wn = kW4Waves / sh.wk, wk = wave % sh.wk;
-  const int tile0 = (cb * wn + wave / sh.wk) * NT;
+  const int wn = kW4Waves / sh.wk, wk = wave % sh.wk, tile0 = (cb * wn + wave / sh.wk) * NT;
   if (cb * wn * NT >= a.tiles) return;
   const int row0 = rb * sh.rows, rows = min(sh.rows, a.M - row0);
 
-  // a K block's codes, scales and zero points for this wave (past the end: some that exist), as they are in memory
+  // a K block's codes, scales and zero points, as they are in memory
   typedef ST scales_t __attribute__((ext_vector_type(GPB)));
   struct Block {
     uint4 code[NT];
@@ -283,9 +285,10 @@ __global__ __launch_bounds__(kW4Threads) __attribute__((amdgpu_waves_per_eu(RT =
     uint32_t zero[NT];
   };
   auto load = [&](Block& b, int kb) {
+    if (kb >= a.kblocks) return;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int64_t tb = (int64_t)min(tile0 + t, a.tiles - 1) * a.kblocks + min(kb, a.kblocks - 1);
+      const int64_t tb = (int64_t)min(tile0 + t, a.tiles - 1) * a.kblocks + kb;
       b.code[t] = (a.codes + tb * 64)[lane];
       b.scale[t] = ((const scales_t*)a.scales + tb * kW4Cols)[r16];
       b.zero[t] = 0x08080808u;
@@ -299,47 +302,91 @@ __global__ __launch_bounds__(kW4Threads) __attribute__((amdgpu_waves_per_eu(RT =
       }
     }
   };
-  const Masks masks;
-  Block b0, b1;
-  load(b0, wk);
-  load(b1, wk + sh.wk);
-
-  // the rows' largest inputs
-  if (tid < kW4MaxRows) row_max[tid] = 0;
-  __syncthreads();
-  const XT* x = (const XT*)a.x + (int64_t)row0 * a.ld_x;
-  // (16 lanes take a K block of a row)
-  auto each_vector = [&](int nkb, auto&& f) {  // f(row, vector of the row)
-    const int dk = kW4Threads / 16 % nkb, dm = kW4Threads / 16 / nkb;
-    int kb = (tid >> 4) % nkb;
-    for (int m = (tid >> 4) / nkb; m < rows; m += dm) {
-      f(m, kb * 16 + r16);
-      kb += dk;
-      if (kb >= nkb) {
-        kb -= nkb;
-        ++m;
-      }
-    }
-  };
-  each_vector(a.kblocks, [&](int m, int kv) {
-    float v[8], mx = 0.f;
-    load8(x + m * a.ld_x + kv * 8, a.K - kv * 8, v);
+  Block ring[D];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float f = fabsf(v[e]);
-      mx = f < INFINITY ? fmaxf(mx, f) : mx;
+  for (int d = 0; d < D; ++d) load(ring[d], d * sh.wk + wk);
+  float bias[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) bias[t] = a.bias ? a.bias[min(tile0 + t, a.tiles - 1) * kW4Cols + r16] : 0.f;
+
+  // K blocks kb0 .. kb0 + nkb - 1 of the rows to LDS: 16 lanes take one of a row
+  const XT* x = (const XT*)a.x + (int64_t)row0 * a.ld_x;
+  float* units = (float*)(lds + sh.chunk * 16 * HV * RS);
+  auto stage = [&](int kb0, int nkb) {
+    for (int p = tid >> 4; p < rows * nkb; p += kW4Waves * 4) {
+      const int m = p / nkb, kl = p % nkb, k = (kb0 + kl) * kW4Rows + r16 * 8;
+      float v[8], mx = 0.f;
+      load8(x + m * a.ld_x + k, a.K - k, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx = fabsf(v[e]) < INFINITY ? fmaxf(mx, fabsf(v[e])) : mx;
+      mx = max16(mx);
+      // 2^e puts the largest in [2^14, 2^15); e not above 120, so that 2^-e is normal
+      const int e2 = mx > 0.f ? min(15 - __builtin_amdgcn_frexp_expf(mx), 120) : 0;
+      if (r16 == 0) units[kl * (16 * RT) + m] = __builtin_amdgcn_ldexpf(1.f, -e2);
+      const float up = __builtin_amdgcn_ldexpf(1.f, e2);
+      f16x8 hi, lo;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float f = v[e] * up;
+        hi[e] = (_Float16)f;
+        lo[e] = fabsf(f) < INFINITY ? (_Float16)(f - (float)hi[e]) : (_Float16)0.f;  // (an infinity is all in hi)
+      }
+      f32x4* to = lds + ((kl * 4 + (r16 >> 2)) * HV * 4 + (r16 & 3)) * RS + m;
+      to[0] = __builtin_bit_cast(f32x4, hi);
+      if constexpr (HV == 2) to[4 * RS] = __builtin_bit_cast(f32x4, lo);
     }
-    mx = max16(mx);
-    if (r16 == 0) atomicMax(&row_max[m], __builtin_bit_cast(uint32_t, mx));
-  });
-  __syncthreads();
-  // the power of two that puts a row's largest in [2^14, 2^15); not above 2^120, whose reciprocal is normal
-  auto exponent = [&](int m) {
-    const float mx = __builtin_bit_cast(float, row_max[m]);
-    return mx > 0.f ? min(15 - __builtin_amdgcn_frexp_expf(mx), 120) : 0;
   };
 
+  const Masks masks;
   f32x4 sum[NT][RT];
+  auto compute = [&](const Block& b, int kl) {
+    const f32x4* from = lds + (kl * 16 * HV + q) * RS + min(r16, RM - 1);
+    f32x4 acc[NT][RT], part[NT][RT];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      constexpr int kStepsPerGroup = 4 / GPB;
+      const bool first = s % kStepsPerGroup == 0;
+      const int g = s / kStepsPerGroup;
+      f32x4 xf[RT][HV];
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int z = 0; z < HV; ++z) xf[i][z] = from[(s * HV + z) * 4 * RS + i * 16];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        // the group's zero point in both halves; -(1024 + z) and -(64 + z) as bits
+        const uint32_t z = __builtin_amdgcn_perm(0u, b.zero[t], 0x0c000c00u | (uint32_t)g * 0x00010001u);
+        const f16x2 zl = __builtin_bit_cast(f16x2, z | 0xe400e400u);
+        const f16x2 zh = __builtin_bit_cast(f16x2, (z << 4) | 0xd400d400u);
+        const uint32_t w = s == 0 ? b.code[t].x : s == 1 ? b.code[t].y : s == 2 ? b.code[t].z : b.code[t].w;
+        const f16x8 c = codes_f16(w, zl, zh, masks);
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int h = HV - 1; h >= 0; --h)
+            acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, xf[i][h]), c,
+                                                               first && h == HV - 1 ? zero4() : acc[t][i], 0, 0, 0);
+      }
+      if ((s + 1) % kStepsPerGroup == 0)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              part[t][i][e] = g == 0 ? acc[t][i][e] * (float)b.scale[t][g]
+                                     : fmaf(acc[t][i][e], (float)b.scale[t][g], part[t][i][e]);
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const f32x4 unit = *(const f32x4*)(units + kl * (16 * RT) + i * 16 + 4 * q);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[t][i][e] = fmaf(part[t][i][e], unit[e], sum[t][i][e]);
+    }
+  };
+
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -347,73 +394,19 @@ __global__ __launch_bounds__(kW4Threads) __attribute__((amdgpu_waves_per_eu(RT =
   for (int kb0 = 0; kb0 < a.kblocks; kb0 += sh.chunk) {
     const int nkb = min(sh.chunk, a.kblocks - kb0);
     if (kb0 > 0) __syncthreads();
-    each_vector(nkb, [&](int m, int kv) {
-      const int k = kb0 * kW4Rows + kv * 8, e2 = exponent(m);
-      float v[8];
-      load8(x + m * a.ld_x + k, a.K - k, v);
-      f16x8 hi, lo;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float f = __builtin_amdgcn_ldexpf(v[e], e2);
-        hi[e] = (_Float16)f;
-        // (an infinity or NaN is all in hi)
-        lo[e] = fabsf(f) < INFINITY ? (_Float16)(f - (float)hi[e]) : (_Float16)0.f;
-      }
-      f32x4* to = lds + ((kv >> 2) * HV * 4 + (kv & 3)) * rows + m;
-      to[0] = __builtin_bit_cast(f32x4, hi);
-      if constexpr (HV == 2) to[4 * rows] = __builtin_bit_cast(f32x4, lo);
-    });
+    stage(kb0, nkb);
     __syncthreads();
-
-    auto compute = [&](const Block& b, int kl) {
-      const f32x4* from = lds + (kl * 16 * HV + q) * rows;
-      f32x4 acc[NT][RT];
+    for (int k0 = wk; k0 < nkb; k0 += D * sh.wk)
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        constexpr int kStepsPerGroup = 4 / GPB;
-        const bool first = s % kStepsPerGroup == 0;
-        const int g = s / kStepsPerGroup;
-        f32x4 xf[RT][HV];
-#pragma unroll
-        for (int i = 0; i < RT; ++i)
-#pragma unroll
-          for (int z = 0; z < HV; ++z) xf[i][z] = from[(s * HV + z) * 4 * rows + min(i * 16 + r16, rows - 1)];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          // the group's zero point in both halves; -(1024 + z) and -(64 + z) as bits
-          const uint32_t z = __builtin_amdgcn_perm(0u, b.zero[t], 0x0c000c00u | (uint32_t)g * 0x00010001u);
-          const f16x2 zl = __builtin_bit_cast(f16x2, z | 0xe400e400u);
-          const f16x2 zh = __builtin_bit_cast(f16x2, (z << 4) | 0xd400d400u);
-          const uint32_t w = s == 0 ? b.code[t].x : s == 1 ? b.code[t].y : s == 2 ? b.code[t].z : b.code[t].w;
-          const f16x8 c = codes_f16(w, zl, zh, masks);
-#pragma unroll
-          for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int h = HV - 1; h >= 0; --h)
-              acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, xf[i][h]), c,
-                                                                 first && h == HV - 1 ? zero4() : acc[t][i], 0, 0, 0);
-        }
-        if ((s + 1) % kStepsPerGroup == 0)
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) sum[t][i][e] = fmaf(acc[t][i][e], (float)b.scale[t][g], sum[t][i][e]);
+      for (int d = 0; d < D; ++d) {
+        const int kl = k0 + d * sh.wk;
+        if (kl < nkb) compute(ring[d], kl);
+        load(ring[d], kb0 + kl + D * sh.wk);
       }
-    };
-    for (int kl = wk; kl < nkb; kl += 2 * sh.wk) {
-      compute(b0, kl);
-      load(b0, kb0 + kl + 2 * sh.wk);
-      if (kl + sh.wk >= nkb) break;
-      compute(b1, kl + sh.wk);
-      load(b1, kb0 + kl + 3 * sh.wk);
-    }
   }
 
   if (sh.wk > 1) {  // the K shares' sums, in order
-    __syncthreads();
-    f32x4* red = lds + (wave * NT * RT) * 64 + lane;
+    f32x4* red = lds + sh.chunk * (16 * HV * RS + 4 * RT) + wave * (NT * RT * 64) + lane;
     if (wk > 0)
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -433,61 +426,75 @@ __global__ __launch_bounds__(kW4Threads) __attribute__((amdgpu_waves_per_eu(RT =
     for (int e = 0; e < 4; ++e) {
       const int m = i * 16 + 4 * q + e;
       if (m >= rows) continue;
-      const float unit = __builtin_amdgcn_ldexpf(1.f, -exponent(m));
+      const int64_t at = (row0 + m) * a.ld_y + r16;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const int64_t n = (int64_t)(tile0 + t) * kW4Cols + r16, at = (int64_t)(row0 + m) * a.ld_y + n;
-        if (n >= a.N) continue;
-        const float y = fmaf(sum[t][i][e], unit, a.bias ? a.bias[n] : 0.f);
+        const int n = (tile0 + t) * kW4Cols;
+        if (n + r16 >= a.N) continue;
         if (a.y16)
-          ((__bf16*)a.y)[at] = (__bf16)y;
+          ((__bf16*)a.y)[at + n] = (__bf16)(sum[t][i][e] + bias[t]);
         else
-          ((float*)a.y)[at] = y;
+          ((float*)a.y)[at + n] = sum[t][i][e] + bias[t];
       }
     }
 }
 
-template <int RT, int NT, int GPB, bool X16, bool S16>
+// Bytes of LDS that a K block takes.
+constexpr int w4_block_bytes(int RM, bool x16) { return (RM + 1) * (x16 ? 256 : 512) + (RM + 15) / 16 * 64; }
+
+template <int RM, int NT, int GPB, bool X16, bool S16>
 hipError_t launch_form(const W4Args& a, const W4Shape& sh, hipStream_t st) {
-  const int wn = kW4Waves / sh.wk;
-  const int64_t cbs = round_up(ceil_div(a.tiles, wn * NT), 8), grid = cbs * sh.row_blocks;
+  const int64_t grid = round_up(ceil_div(a.tiles, kW4Waves / sh.wk * NT), 8) * sh.row_blocks;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  // a chunk's fragments, or the K shares' sums
-  const size_t frag = (size_t)std::min(sh.rows, a.M) * sh.chunk * 16 * (X16 ? 16 : 32);
-  const size_t red = sh.wk > 1 ? (size_t)kW4Waves * NT * RT * 64 * 16 : 0;
-  hipLaunchKernelGGL((k_w4_product<RT, NT, GPB, X16, S16>), dim3((unsigned)grid), dim3(kW4Threads), std::max(frag, red),
-                     st, a, sh);
+  const size_t lds = (size_t)sh.chunk * w4_block_bytes(RM, X16) +
+                     (sh.wk > 1 ? (size_t)kW4Waves * NT * ((RM + 15) / 16) * 64 * 16 : 0);
+  hipLaunchKernelGGL((k_w4_product<RM, NT, GPB, X16, S16>), dim3((unsigned)grid), dim3(kW4Waves * 64), lds, st, a, sh);
   return hipGetLastError();
 }
 
 hipError_t launch_product(const W4Args& a, bool x16, bool s16, int gpb, int cus, hipStream_t st) {
-  // rows evenly over blocks of at most 64
+  // Rows a block: as many as leave enough column pairs for four waves a CU.
   W4Shape sh{};
-  sh.row_blocks = ceil_div(a.M, kW4MaxRows);
-  const int rt16 = ceil_div(ceil_div(a.M, sh.row_blocks), 16), RT = rt16 > 2 ? 4 : rt16;
-  sh.rows = a.M < 16 ? a.M : rt16 * 16;
-  // K blocks of the largest chunk; K split between waves while there are fewer than about 8 waves a CU
-  const int most = std::min(kStageVectors / 16 / sh.rows, a.kblocks);
-  const int NT = RT == 1 && a.tiles < 4 * cus ? 1 : 2;
+  const int tiles16 = ceil_div(a.M, 16);
+  auto groups_of = [&](int rt) { return (int64_t)ceil_div(a.tiles, 2) * ceil_div(tiles16, rt); };
+  int RT = std::min(tiles16, 4);
+  while (RT > 1 && groups_of(RT) < 4 * cus) --RT;
+  sh.row_blocks = ceil_div(tiles16, RT);
+  RT = ceil_div(tiles16, sh.row_blocks);
+  sh.rows = std::min(a.M, RT * 16);
+  const int RM = a.M <= 4 ? 4 : RT * 16, NT = RT == 1 && groups_of(1) < 8 * cus ? 1 : 2;
+  // LDS: one block a CU with many rows, two with few
+  const int most = std::max(1, (RT > 2 ? 128 << 10 : 56 << 10) / w4_block_bytes(RM, x16));
+  // K split between waves while there are fewer than about 8 waves a CU (and little to add up)
+  const int64_t groups = (int64_t)ceil_div(a.tiles, NT) * sh.row_blocks;
   sh.wk = 1;
-  while (sh.wk < kW4Waves && (sh.wk * 4 <= most || (most == a.kblocks && sh.wk * 2 <= most)) &&
-         (int64_t)ceil_div(a.tiles, NT) * sh.row_blocks * sh.wk < 8 * cus)
+  while (RT <= 2 && sh.wk < kW4Waves && groups * sh.wk < 8 * cus &&
+         (most >= a.kblocks ? sh.wk * 2 <= a.kblocks : sh.wk * 2 * w4_depth(RM) <= most))
     sh.wk *= 2;
-  sh.chunk = most == a.kblocks ? most : most / (2 * sh.wk) * (2 * sh.wk);
-  auto types = [&](auto rt, auto nt, auto g) {
-    constexpr int R = decltype(rt)::value, T = decltype(nt)::value, G = decltype(g)::value;
+  const int step = w4_depth(RM) * sh.wk;
+  sh.chunk = most >= a.kblocks ? a.kblocks : most / step * step;
+  auto types = [&](auto rm, auto nt, auto g) {
+    constexpr int R = decltype(rm)::value, T = decltype(nt)::value, G = decltype(g)::value;
     return x16 ? (s16 ? launch_form<R, T, G, true, true>(a, sh, st) : launch_form<R, T, G, true, false>(a, sh, st))
                : (s16 ? launch_form<R, T, G, false, true>(a, sh, st) : launch_form<R, T, G, false, false>(a, sh, st));
   };
-  auto groups = [&](auto rt, auto nt) {
-    return gpb == 4   ? types(rt, nt, std::integral_constant<int, 4>{})
-           : gpb == 2 ? types(rt, nt, std::integral_constant<int, 2>{})
-                      : types(rt, nt, std::integral_constant<int, 1>{});
+  auto groups_form = [&](auto rm, auto nt) {
+    return gpb == 4   ? types(rm, nt, std::integral_constant<int, 4>{})
+           : gpb == 2 ? types(rm, nt, std::integral_constant<int, 2>{})
+                      : types(rm, nt, std::integral_constant<int, 1>{});
   };
-  constexpr std::integral_constant<int, 1> I1{};
-  constexpr std::integral_constant<int, 2> I2{};
-  constexpr std::integral_constant<int, 4> I4{};
-  return RT == 1 ? (NT == 1 ? groups(I1, I1) : groups(I1, I2)) : RT == 2 ? groups(I2, I2) : groups(I4, I2);
+  auto form = [&](auto rm) {
+    if constexpr (decltype(rm)::value <= 16)
+      if (NT == 1) return groups_form(rm, std::integral_constant<int, 1>{});
+    return groups_form(rm, std::integral_constant<int, 2>{});
+  };
+  switch (RM) {
+    case 4: return form(std::integral_constant<int, 4>{});
+    case 16: return form(std::integral_constant<int, 16>{});
+    case 32: return form(std::integral_constant<int, 32>{});
+    case 48: return form(std::integral_constant<int, 48>{});
+    default: return form(std::integral_constant<int, 64>{});
+  }
 }
 
 bool known_type(int32_t t) { return t == NMT_F32 || t == NMT_BF16; }
