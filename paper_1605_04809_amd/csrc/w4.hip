@@ -168,19 +168,20 @@ __global__ __launch_bounds__(256) void k_w4_out_codes(const void* __restrict__ W
 // by the MFMA, then times the scale to the block's sum and times 2^-e to the
 // row's.
 //
-// A block of 8 waves takes up to RM rows and 8 NT / WK column tiles.  It holds
-// the rows' inputs in LDS as MFMA fragments, converted once a block (K too long
-// for LDS is taken in chunks).  The codes stream from memory straight into
-// registers, D K blocks ahead and from before the inputs are converted, each 16-byte vector the operand of four MFMA steps
-// of 32 rows of W: 9 instructions turn a 32-bit word into eight fp16 values
+// A block takes up to RM rows, holds their inputs in LDS as MFMA fragments,
+// converted once a block (K too long for LDS is taken in chunks), and walks over
+// the column tiles, one for each group of WK waves at a time.  The codes stream
+// from memory straight into registers, D K blocks ahead and from before the
+// inputs are converted, each 16-byte vector the operand of four MFMA steps of
+// 32 rows of W: 9 instructions turn a 32-bit word into eight fp16 values
 // (0x6400 | n is 1024 + n; the upper nibble of a byte, in place, gives
 // 1024 + 16 n).  Lane 16 q + r holds column r of a tile, so it needs one scale
 // and one zero point a group.  WK > 1 splits K between waves where there are
 // few columns; their sums meet in LDS in a fixed order.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kW4Waves = 8;
 
 struct W4Args {
   const uint4* codes;
@@ -194,12 +195,19 @@ struct W4Args {
   void* y;
   int64_t ld_y;
 };
-// How a launch is cut: rows a block (at most RM), row blocks, waves that share
-// a column's K, K blocks a chunk (a multiple of D wk, or all).
+// How a launch is cut: rows a block (at most RM), row blocks, blocks that share
+// a row block's columns (a multiple of 8), waves that share a column's K, K
+// blocks a chunk (a multiple of D wk, or all).
 struct W4Shape {
-  int rows, row_blocks, wk, chunk;
+  int rows, row_blocks, strips, wk, chunk;
 };
-constexpr int w4_depth(int RM) { return RM <= 16 ? 4 : 2; }  // K blocks in flight
+// Waves a block, and K blocks in flight.  Many rows fill a CU's LDS by
+// themselves, so their block is 16 waves (80 rows of K = 500, N = 100,000: 51
+// us with 8, 32 with 16); few leave room for two blocks, and a wave for the
+// whole K of an output layer (33 rows of 1001 x 7777: 10.1 us with two K blocks
+// in flight, 9.1 with four).
+constexpr int w4_waves(int RM) { return RM > 16 ? 16 : 8; }
+constexpr int w4_depth(int RM, int GPB) { return RM > 16 || (RM == 16 && GPB == 4) ? 2 : 4; }
 
 // Eight codes of a word as fp16, minus the zero point: zl = -(1024 + z) and
 // zh = -(64 + z), twice each.  (The masks sit in registers, or the compiler
@@ -256,244 +264,276 @@ __device__ __forceinline__ float max16(float v) {
   return v;
 }
 
-template <int RM, int NT, int GPB, bool X16, bool S16>
-__global__ __launch_bounds__(kW4Waves * 64) __attribute__((amdgpu_waves_per_eu(RM > 32 ? 2 : 4))) void k_w4_product(
+template <int RM, int GPB, bool X16, bool S16>
+__global__ __launch_bounds__(w4_waves(RM) * 64) __attribute__((amdgpu_waves_per_eu(4))) void k_w4_product(
     W4Args a, W4Shape sh) {
-  constexpr int RT = (RM + 15) / 16, RS = RM + 1;  // row tiles; rows of an LDS fragment (odd, a constant: its steps
-                                                   // are offsets within the instructions)
+  constexpr int RT = (RM + 15) / 16;  // row tiles
   constexpr int HV = X16 ? 1 : 2;  // fp16 parts of an input
-  constexpr int D = w4_depth(RM);
+  constexpr int D = w4_depth(RM, GPB), W = w4_waves(RM);
   using XT = std::conditional_t<X16, __bf16, float>;
   using ST = std::conditional_t<S16, __bf16, float>;
-  // [K block][step][part][lane quarter][row] fragments, then
+  // [K block][step][part][lane quarter][row ^ (4 step + quarter)] fragments
+  // (rows permuted within their tile, so that the 16 lanes that write one
+  // row's vectors do not meet in one bank; RM = 4 keeps them in order), then
   // [K block][16 RT] 2^-e, then the K shares' sums
   extern __shared__ f32x4 lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, q = lane >> 4;
   // the row blocks of the same columns run on one XCD, whose L2 then holds their codes
   const int id = blockIdx.x, slot = id >> 3;
-  const int cb = (slot / sh.row_blocks) * 8 + (id & 7), rb = slot % sh.row_blocks;
-  const int wn = kW4Waves / sh.wk, wk = wave % sh.wk, tile0 = (cb * wn + wave / sh.wk) * NT;
-  if (cb * wn * NT >= a.tiles) return;
+  const int strip = (slot / sh.row_blocks) * 8 + (id & 7), rb = slot % sh.row_blocks;
+  const int wk = wave % sh.wk, per_block = W / sh.wk;  // tiles
   const int row0 = rb * sh.rows, rows = min(sh.rows, a.M - row0);
 
   // a K block's codes, scales and zero points, as they are in memory
   typedef ST scales_t __attribute__((ext_vector_type(GPB)));
   struct Block {
-    uint4 code[NT];
-    scales_t scale[NT];
-    uint32_t zero[NT];
+    uint4 code;
+    scales_t scale;
+    uint32_t zero;
   };
-  auto load = [&](Block& b, int kb) {
-    if (kb >= a.kblocks) return;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int64_t tb = (int64_t)min(tile0 + t, a.tiles - 1) * a.kblocks + kb;
-      b.code[t] = (a.codes + tb * 64)[lane];
-      b.scale[t] = ((const scales_t*)a.scales + tb * kW4Cols)[r16];
-      b.zero[t] = 0x08080808u;
-      if (a.zeros) {
-        if constexpr (GPB == 4)
-          b.zero[t] = ((const uint32_t*)a.zeros + tb * kW4Cols)[r16];
-        else if constexpr (GPB == 2)
-          b.zero[t] = ((const uint16_t*)a.zeros + tb * kW4Cols)[r16];
-        else
-          b.zero[t] = (a.zeros + tb * kW4Cols)[r16];
-      }
+  auto load = [&](Block& b, int tile, int kb) {
+    if (tile >= a.tiles || kb >= a.kblocks) return;
+    const int64_t tb = (int64_t)tile * a.kblocks + kb;
+    b.code = (a.codes + tb * 64)[lane];
+    b.scale = ((const scales_t*)a.scales + tb * kW4Cols)[r16];
+    b.zero = 0x08080808u;
+    if (a.zeros) {
+      if constexpr (GPB == 4)
+        b.zero = ((const uint32_t*)a.zeros + tb * kW4Cols)[r16];
+      else if constexpr (GPB == 2)
+        b.zero = ((const uint16_t*)a.zeros + tb * kW4Cols)[r16];
+      else
+        b.zero = (a.zeros + tb * kW4Cols)[r16];
     }
   };
+  const int tile_step = sh.strips * per_block;
+  int tile = strip * per_block + wave / sh.wk;
   Block ring[D];
 #pragma unroll
-  for (int d = 0; d < D; ++d) load(ring[d], d * sh.wk + wk);
-  float bias[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) bias[t] = a.bias ? a.bias[min(tile0 + t, a.tiles - 1) * kW4Cols + r16] : 0.f;
+  for (int d = 0; d < D; ++d) load(ring[d], tile, d * sh.wk + wk);
 
-  // K blocks kb0 .. kb0 + nkb - 1 of the rows to LDS: 16 lanes take one of a row
-  const XT* x = (const XT*)a.x + (int64_t)row0 * a.ld_x;
-  float* units = (float*)(lds + sh.chunk * 16 * HV * RS);
-  auto stage = [&](int kb0, int nkb) {
-    for (int p = tid >> 4; p < rows * nkb; p += kW4Waves * 4) {
-      const int m = p / nkb, kl = p % nkb, k = (kb0 + kl) * kW4Rows + r16 * 8;
-      float v[8], mx = 0.f;
-      load8(x + m * a.ld_x + k, a.K - k, v);
+  // Eight inputs of a K block that 16 lanes hold to LDS; returns the block's 2^-e
+  auto convert = [&](const float (&v)[8], f32x4* to) {
+    float mx = 0.f;  // (fmaxf passes over NaN, which is NaN at any scale)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(v[e]));
+    mx = max16(mx);
+    const bool infinite = __ballot(mx == INFINITY) != 0;
+    if (infinite) {  // the largest of the finite ones
+      mx = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) mx = fabsf(v[e]) < INFINITY ? fmaxf(mx, fabsf(v[e])) : mx;
       mx = max16(mx);
-      // 2^e puts the largest in [2^14, 2^15); e not above 120, so that 2^-e is normal
-      const int e2 = mx > 0.f ? min(15 - __builtin_amdgcn_frexp_expf(mx), 120) : 0;
-      if (r16 == 0) units[kl * (16 * RT) + m] = __builtin_amdgcn_ldexpf(1.f, -e2);
-      const float up = __builtin_amdgcn_ldexpf(1.f, e2);
-      f16x8 hi, lo;
+    }
+    // 2^e puts the largest in [2^14, 2^15); e not above 120, so that 2^-e is normal
+    const int e2 = mx > 0.f ? min(15 - __builtin_amdgcn_frexp_expf(mx), 120) : 0;
+    const float up = __builtin_amdgcn_ldexpf(1.f, e2);
+    f16x8 hi, lo;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float f = v[e] * up;
-        hi[e] = (_Float16)f;
-        lo[e] = fabsf(f) < INFINITY ? (_Float16)(f - (float)hi[e]) : (_Float16)0.f;  // (an infinity is all in hi)
+    for (int e = 0; e < 8; e += 2) {
+      f32x2 f;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f[u] = v[e + u] * up;
+        // (kept in a register, or it is rounded to fp16 a second time for the remainder)
+        if constexpr (HV == 2) asm("" : "+v"(f[u]));
       }
-      f32x4* to = lds + ((kl * 4 + (r16 >> 2)) * HV * 4 + (r16 & 3)) * RS + m;
-      to[0] = __builtin_bit_cast(f32x4, hi);
-      if constexpr (HV == 2) to[4 * RS] = __builtin_bit_cast(f32x4, lo);
+      const f16x2 h = __builtin_convertvector(f, f16x2);
+      hi[e] = h[0];
+      hi[e + 1] = h[1];
+      if constexpr (HV == 2) {
+        lo[e] = (_Float16)(f[0] - (float)h[0]);
+        lo[e + 1] = (_Float16)(f[1] - (float)h[1]);
+      }
+    }
+    if constexpr (HV == 2)
+      if (infinite)  // an infinity is all in hi (inf - inf is no remainder)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) lo[e] = fabsf(v[e]) < INFINITY ? lo[e] : (_Float16)0.f;
+    to[0] = __builtin_bit_cast(f32x4, hi);
+    if constexpr (HV == 2) to[4 * RM] = __builtin_bit_cast(f32x4, lo);
+    return __builtin_amdgcn_ldexpf(1.f, -e2);
+  };
+  // K blocks kb0 .. kb0 + nkb - 1 of the rows to LDS: 16 lanes take one of a
+  // row, U of them at a time so that their loads are in flight together
+  constexpr int U = RM <= 4 ? 1 : RM <= 16 ? 2 : 4, kTakers = W * 4;
+  const XT* x = (const XT*)a.x + (int64_t)row0 * a.ld_x;
+  float* units = (float*)(lds + sh.chunk * 16 * HV * RM);
+  auto stage = [&](int kb0, int nkb) {
+    for (int p0 = tid >> 4; p0 < rows * nkb; p0 += U * kTakers) {
+      float v[U][8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int p = p0 + u * kTakers, m = p / nkb, k = (kb0 + p % nkb) * kW4Rows + r16 * 8;
+        load8(x + m * a.ld_x + k, p < rows * nkb ? a.K - k : 0, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int p = p0 + u * kTakers, m = p / nkb, kl = p % nkb;
+        if (p >= rows * nkb) break;
+        f32x4* to = lds + ((kl * 4 + (r16 >> 2)) * HV * 4 + (r16 & 3)) * RM + (RM < 16 ? m : m ^ r16);
+        const float unit = convert(v[u], to);
+        if (r16 == 0) units[kl * (16 * RT) + m] = unit;
+      }
     }
   };
 
   const Masks masks;
-  f32x4 sum[NT][RT];
+  int x_row[4];  // where the lane's row of a step's fragments lies
+#pragma unroll
+  for (int s = 0; s < 4; ++s) x_row[s] = RM < 16 ? min(r16, RM - 1) : r16 ^ (4 * s + q);
+  f32x4 sum[RT];
   auto compute = [&](const Block& b, int kl) {
-    const f32x4* from = lds + (kl * 16 * HV + q) * RS + min(r16, RM - 1);
-    f32x4 acc[NT][RT], part[NT][RT];
+    const f32x4* from = lds + (kl * 16 * HV + q) * RM;
+    f32x4 acc[RT], part[RT], xf[2][RT][HV];
+    auto fetch = [&](int s) {  // a step ahead of its products
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int z = 0; z < HV; ++z) xf[s & 1][i][z] = (from + x_row[s])[(s * HV + z) * 4 * RM + i * 16];
+    };
+    fetch(0);
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       constexpr int kStepsPerGroup = 4 / GPB;
       const bool first = s % kStepsPerGroup == 0;
       const int g = s / kStepsPerGroup;
-      f32x4 xf[RT][HV];
+      if (s < 3) fetch(s + 1);
+      // the group's zero point in both halves; -(1024 + z) and -(64 + z) as bits
+      const uint32_t z = __builtin_amdgcn_perm(0u, b.zero, 0x0c000c00u | (uint32_t)g * 0x00010001u);
+      const f16x2 zl = __builtin_bit_cast(f16x2, z | 0xe400e400u);
+      const f16x2 zh = __builtin_bit_cast(f16x2, (z << 4) | 0xd400d400u);
+      const uint32_t w = s == 0 ? b.code.x : s == 1 ? b.code.y : s == 2 ? b.code.z : b.code.w;
+      const f16x8 c = codes_f16(w, zl, zh, masks);
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int h = HV - 1; h >= 0; --h)
 #pragma unroll
-        for (int z = 0; z < HV; ++z) xf[i][z] = from[(s * HV + z) * 4 * RS + i * 16];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        // the group's zero point in both halves; -(1024 + z) and -(64 + z) as bits
-        const uint32_t z = __builtin_amdgcn_perm(0u, b.zero[t], 0x0c000c00u | (uint32_t)g * 0x00010001u);
-        const f16x2 zl = __builtin_bit_cast(f16x2, z | 0xe400e400u);
-        const f16x2 zh = __builtin_bit_cast(f16x2, (z << 4) | 0xd400d400u);
-        const uint32_t w = s == 0 ? b.code[t].x : s == 1 ? b.code[t].y : s == 2 ? b.code[t].z : b.code[t].w;
-        const f16x8 c = codes_f16(w, zl, zh, masks);
+        for (int i = 0; i < RT; ++i)
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, xf[s & 1][i][h]), c,
+                                                          first && h == HV - 1 ? zero4() : acc[i], 0, 0, 0);
+      if ((s + 1) % kStepsPerGroup == 0)
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
-          for (int h = HV - 1; h >= 0; --h)
-            acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, xf[i][h]), c,
-                                                               first && h == HV - 1 ? zero4() : acc[t][i], 0, 0, 0);
-      }
-      if ((s + 1) % kStepsPerGroup == 0)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              part[t][i][e] = g == 0 ? acc[t][i][e] * (float)b.scale[t][g]
-                                     : fmaf(acc[t][i][e], (float)b.scale[t][g], part[t][i][e]);
+          for (int e = 0; e < 4; ++e)
+            part[i][e] = g == 0 ? acc[i][e] * (float)b.scale[g] : fmaf(acc[i][e], (float)b.scale[g], part[i][e]);
     }
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
       const f32x4 unit = *(const f32x4*)(units + kl * (16 * RT) + i * 16 + 4 * q);
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[t][i][e] = fmaf(part[t][i][e], unit[e], sum[t][i][e]);
+      for (int e = 0; e < 4; ++e) sum[i][e] = fmaf(part[i][e], unit[e], sum[i][e]);
     }
   };
 
+  f32x4* red = lds + sh.chunk * (16 * HV * RM + 4 * RT) + wave * (RT * 64) + lane;
+  // every wave goes round as often as the block's first has tiles
+  for (int first = strip * per_block; first < a.tiles; first += tile_step, tile += tile_step) {
+    const float bias = a.bias && tile < a.tiles ? a.bias[tile * kW4Cols + r16] : 0.f;
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int i = 0; i < RT; ++i) sum[t][i] = zero4();
-  for (int kb0 = 0; kb0 < a.kblocks; kb0 += sh.chunk) {
-    const int nkb = min(sh.chunk, a.kblocks - kb0);
-    if (kb0 > 0) __syncthreads();
-    stage(kb0, nkb);
-    __syncthreads();
-    for (int k0 = wk; k0 < nkb; k0 += D * sh.wk)
-#pragma unroll
-      for (int d = 0; d < D; ++d) {
-        const int kl = k0 + d * sh.wk;
-        if (kl < nkb) compute(ring[d], kl);
-        load(ring[d], kb0 + kl + D * sh.wk);
+    for (int i = 0; i < RT; ++i) sum[i] = zero4();
+    for (int kb0 = 0; kb0 < a.kblocks; kb0 += sh.chunk) {
+      const int nkb = min(sh.chunk, a.kblocks - kb0);
+      if (sh.chunk < a.kblocks || first < tile_step) {  // (all of K stays from the first time on)
+        if (first >= tile_step || kb0 > 0) __syncthreads();
+        stage(kb0, nkb);
+        __syncthreads();
       }
-  }
-
-  if (sh.wk > 1) {  // the K shares' sums, in order
-    f32x4* red = lds + sh.chunk * (16 * HV * RS + 4 * RT) + wave * (NT * RT * 64) + lane;
-    if (wk > 0)
+      for (int j = 0; j < nkb; j += D * sh.wk) {
+        // what comes after a slot's K block: one of these tiles, or of the next
+        const bool more = kb0 + j + D * sh.wk < a.kblocks;
+        const int next_tile = more ? tile : tile + tile_step, next_kb = more ? kb0 + j + D * sh.wk : 0;
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < RT; ++i) red[(t * RT + i) * 64] = sum[t][i];
-    __syncthreads();
-    if (wk > 0) return;
-    for (int w = 1; w < sh.wk; ++w)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < RT; ++i) sum[t][i] += red[(w * NT * RT + t * RT + i) * 64];
-  }
-#pragma unroll
-  for (int i = 0; i < RT; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int m = i * 16 + 4 * q + e;
-      if (m >= rows) continue;
-      const int64_t at = (row0 + m) * a.ld_y + r16;
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const int n = (tile0 + t) * kW4Cols;
-        if (n + r16 >= a.N) continue;
-        if (a.y16)
-          ((__bf16*)a.y)[at + n] = (__bf16)(sum[t][i][e] + bias[t]);
-        else
-          ((float*)a.y)[at + n] = sum[t][i][e] + bias[t];
+        for (int d = 0; d < D; ++d) {
+          const int kl = j + d * sh.wk + wk;
+          if (kl < nkb && tile < a.tiles) compute(ring[d], kl);
+          load(ring[d], next_tile, next_kb + d * sh.wk + wk);
+        }
       }
     }
+    if (sh.wk > 1) {  // the K shares' sums, in order
+      if (first >= tile_step) __syncthreads();
+      if (wk > 0)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) red[i * 64] = sum[i];
+      __syncthreads();
+      if (wk > 0) continue;
+      for (int w = 1; w < sh.wk; ++w)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) sum[i] += red[(w * RT + i) * 64];
+    }
+    auto store = [&](auto* y) {
+      using YT = std::remove_pointer_t<decltype(y)>;
+      y += (row0 + 4 * q) * a.ld_y + (int64_t)tile * kW4Cols + r16;
+      const int left = rows - 4 * q, cols = a.N - tile * kW4Cols - r16;
+#pragma unroll
+      for (int i = 0; i < RT; ++i, y += 12 * a.ld_y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e, y += a.ld_y)
+          if (i * 16 + e < left && cols > 0) *y = (YT)(sum[i][e] + bias);
+    };
+    if (a.y16)
+      store((__bf16*)a.y);
+    else
+      store((float*)a.y);
+  }
 }
 
 // Bytes of LDS that a K block takes.
-constexpr int w4_block_bytes(int RM, bool x16) { return (RM + 1) * (x16 ? 256 : 512) + (RM + 15) / 16 * 64; }
+constexpr int w4_block_bytes(int RM, bool x16) { return RM * (x16 ? 256 : 512) + (RM + 15) / 16 * 64; }
 
-template <int RM, int NT, int GPB, bool X16, bool S16>
+template <int RM, int GPB, bool X16, bool S16>
 hipError_t launch_form(const W4Args& a, const W4Shape& sh, hipStream_t st) {
-  const int64_t grid = round_up(ceil_div(a.tiles, kW4Waves / sh.wk * NT), 8) * sh.row_blocks;
+  const int64_t grid = (int64_t)sh.strips * sh.row_blocks;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   const size_t lds = (size_t)sh.chunk * w4_block_bytes(RM, X16) +
-                     (sh.wk > 1 ? (size_t)kW4Waves * NT * ((RM + 15) / 16) * 64 * 16 : 0);
-  hipLaunchKernelGGL((k_w4_product<RM, NT, GPB, X16, S16>), dim3((unsigned)grid), dim3(kW4Waves * 64), lds, st, a, sh);
+                     (sh.wk > 1 ? (size_t)w4_waves(RM) * ((RM + 15) / 16) * 64 * 16 : 0);
+  hipLaunchKernelGGL((k_w4_product<RM, GPB, X16, S16>), dim3((unsigned)grid), dim3(w4_waves(RM) * 64), lds, st, a, sh);
   return hipGetLastError();
 }
 
 hipError_t launch_product(const W4Args& a, bool x16, bool s16, int gpb, int cus, hipStream_t st) {
-  // Rows a block: as many as leave enough column pairs for four waves a CU.
+  // Row tiles a block: two, or three where those are all (48 rows of K = 500, N
+  // = 100,000: 19.5 us in one block, 25 in two; more rows take as long either
+  // way, and a fourth tile makes the waves spill), but only one while that
+  // leaves fewer than eight waves a CU.
   W4Shape sh{};
   const int tiles16 = ceil_div(a.M, 16);
-  auto groups_of = [&](int rt) { return (int64_t)ceil_div(a.tiles, 2) * ceil_div(tiles16, rt); };
-  int RT = std::min(tiles16, 4);
-  while (RT > 1 && groups_of(RT) < 4 * cus) --RT;
+  auto groups_of = [&](int rt) { return (int64_t)a.tiles * ceil_div(tiles16, rt); };
+  int RT = tiles16 <= 3 ? tiles16 : 2;
+  while (RT > 1 && groups_of(RT) < 8 * cus) --RT;
   sh.row_blocks = ceil_div(tiles16, RT);
   RT = ceil_div(tiles16, sh.row_blocks);
   sh.rows = std::min(a.M, RT * 16);
-  const int RM = a.M <= 4 ? 4 : RT * 16, NT = RT == 1 && groups_of(1) < 8 * cus ? 1 : 2;
-  // LDS: one block a CU with many rows, two with few
-  const int most = std::max(1, (RT > 2 ? 128 << 10 : 56 << 10) / w4_block_bytes(RM, x16));
-  // K split between waves while there are fewer than about 8 waves a CU (and little to add up)
-  const int64_t groups = (int64_t)ceil_div(a.tiles, NT) * sh.row_blocks;
+  const int RM = a.M <= 4 ? 4 : RT * 16, W = w4_waves(RM), depth = w4_depth(RM, gpb), per_cu = W > 8 ? 1 : 2;
+  const int most = std::max(1, ((per_cu == 1 ? 128 : 56) << 10) / w4_block_bytes(RM, x16));
+  // K split between waves while there are fewer than about 8 waves a CU
+  const int64_t groups = groups_of(RT);
   sh.wk = 1;
-  while (RT <= 2 && sh.wk < kW4Waves && groups * sh.wk < 8 * cus &&
-         (most >= a.kblocks ? sh.wk * 2 <= a.kblocks : sh.wk * 2 * w4_depth(RM) <= most))
+  while (sh.wk < 8 && groups * sh.wk < 8 * cus &&
+         (most >= a.kblocks ? sh.wk * 2 <= a.kblocks : sh.wk * 2 * depth <= most))
     sh.wk *= 2;
-  const int step = w4_depth(RM) * sh.wk;
+  const int step = depth * sh.wk;
   sh.chunk = most >= a.kblocks ? a.kblocks : most / step * step;
-  auto types = [&](auto rm, auto nt, auto g) {
-    constexpr int R = decltype(rm)::value, T = decltype(nt)::value, G = decltype(g)::value;
-    return x16 ? (s16 ? launch_form<R, T, G, true, true>(a, sh, st) : launch_form<R, T, G, true, false>(a, sh, st))
-               : (s16 ? launch_form<R, T, G, false, true>(a, sh, st) : launch_form<R, T, G, false, false>(a, sh, st));
-  };
-  auto groups_form = [&](auto rm, auto nt) {
-    return gpb == 4   ? types(rm, nt, std::integral_constant<int, 4>{})
-           : gpb == 2 ? types(rm, nt, std::integral_constant<int, 2>{})
-                      : types(rm, nt, std::integral_constant<int, 1>{});
+  // as many blocks as run at once, evenly loaded
+  const int want = ceil_div(a.tiles, W / sh.wk), fit = std::max(1, per_cu * cus / sh.row_blocks);
+  sh.strips = (int)round_up(ceil_div(want, ceil_div(want, fit)), 8);
+  auto types = [&](auto rm, auto g) {
+    constexpr int R = decltype(rm)::value, G = decltype(g)::value;
+    return x16 ? (s16 ? launch_form<R, G, true, true>(a, sh, st) : launch_form<R, G, true, false>(a, sh, st))
+               : (s16 ? launch_form<R, G, false, true>(a, sh, st) : launch_form<R, G, false, false>(a, sh, st));
   };
   auto form = [&](auto rm) {
-    if constexpr (decltype(rm)::value <= 16)
-      if (NT == 1) return groups_form(rm, std::integral_constant<int, 1>{});
-    return groups_form(rm, std::integral_constant<int, 2>{});
+    return gpb == 4   ? types(rm, std::integral_constant<int, 4>{})
+           : gpb == 2 ? types(rm, std::integral_constant<int, 2>{})
+                      : types(rm, std::integral_constant<int, 1>{});
   };
   switch (RM) {
     case 4: return form(std::integral_constant<int, 4>{});
     case 16: return form(std::integral_constant<int, 16>{});
     case 32: return form(std::integral_constant<int, 32>{});
-    case 48: return form(std::integral_constant<int, 48>{});
-    default: return form(std::integral_constant<int, 64>{});
+    default: return form(std::integral_constant<int, 48>{});
   }
 }
 
