@@ -12,24 +12,29 @@
 // comparison is in 64 bits: each row's sum of exponentials, the residual's
 // running sum.
 //
-// Large vocabularies take four launches.  k_row_sums reads every row once: a
-// wave takes 2,048 logits of one row into registers, all loads in flight at
-// once, and leaves their (max, sum) pair.  k_judge merges a sequence's pairs
-// and finds where it ends.  k_residual sums what is left of the target over
-// 1,024 words a wave, and k_next finds the part, then the word, whose running
-// sum passes the random number.  Each stage is spread over the whole chip, so
-// one sequence takes no longer than its share of the bandwidth; every sum has
-// a fixed order.  Small ones take one launch, a block a sequence (k_verify_small).
+// Large vocabularies take two launches.  k_row_sums reads every row once: a
+// wave takes up to 2,048 logits into registers, all loads in flight at once, a
+// block leaves a (max, sum) pair for its up to 8,192.  k_finish judges its
+// sequence from those pairs (each block by itself: 16 lanes merge a row, then a
+// lane decides a position), sums what is left of the target over its share of
+// the words, 512 at a time, and the sequence's last block to finish finds the
+// 512, then the word, whose running sum passes the random number.  Both stages
+// are spread over the whole chip, so one sequence takes no longer than its
+// share of the bandwidth; every sum has a fixed order.  Small vocabularies take
+// one launch, a block a sequence (k_verify_small).
+#include <algorithm>
+
 #include "draft.hpp"
 
 using namespace nmt;
 
 namespace {
 
-constexpr int kPart = 2048;       // logits of a row that one wave sums
-constexpr int kRest = 1024;       // words whose residual one wave sums
+constexpr int kWavePart = 2048;   // logits of a row that one wave sums, at most
 constexpr int kWaves = 4;         // waves a block of the streaming kernels
+constexpr int kUnit = 512;        // words whose residual one wave sums at a time
 constexpr int kJudge = 8;         // positions a block judges at a time
+constexpr int kCUs = 256;
 constexpr int kSmallV = 1024 * 8; // words of the one-launch form: eight a thread
 
 // A row's (or a part's) largest logit and the sum of e^(z - max).  A NaN makes
@@ -44,15 +49,17 @@ __device__ __forceinline__ bool is_distribution(const RowSum& r) {
 
 // Where a sequence's words come to an end.
 struct Verdict {
-  RowSum rt, rp;         // the rows that the next word is drawn from
-  int64_t t_row, p_row;  // (p_row -1: the target's alone)
+  int64_t t_row, p_row;  // the rows that the next word is drawn from (p_row -1: the target's alone)
+  double it, ip;         // one over their sums
+  float mt, mp;
   int32_t kept, bad;     // bad: no word follows (and which bits of the error flag)
   int32_t cut;           // without proposals: the word that p goes without (-1: none)
   int32_t whole;         // the residual holds nothing: p itself
 };
 
 struct VerifyArgs {
-  int S, n_draft, V, parts, rests;  // parts of a row, and of a residual
+  int S, n_draft, V;
+  int parts, part_len, units;     // parts of a row and their length, units of a residual
   const int32_t *off, *draft;
   const void *target, *proposal;  // proposal null: drafts are certain
   int target16, proposal16;
@@ -60,11 +67,11 @@ struct VerifyArgs {
   const float* u;
   int32_t *accepted, *next;
   float *draft_logp, *next_logp;  // nullable
-  // workspace: parts of the target's rows, then the proposal's; a sequence's
-  // verdict; its residual's parts
+  // workspace: parts of the target's rows, then the proposal's; units of the
+  // sequences' residuals; blocks of a sequence that have finished
   RowSum* rows;
-  Verdict* verdict;
   double* rest;
+  uint32_t* done;
   int* err;
 };
 
@@ -72,18 +79,17 @@ __device__ __forceinline__ float logit(const void* z, int is16, int64_t i) {
   return is16 ? (float)((const __bf16*)z)[i] : ((const float*)z)[i];
 }
 
-// e^x for x <= 0 as 2^n e^r, |r| <= ln 2 / 2, e^r by the polynomial that
+// e^x as 2^n e^r, |r| <= ln 2 / 2, e^r by the polynomial that
 // interpolates it at the Chebyshev nodes (off by at most 5.6e-11 of it, and
-// exact at 0).  15 64-bit instructions a logit, each at the rate of a 64-bit
+// exact at 0).  14 64-bit instructions a logit, each at the rate of a 64-bit
 // multiply-add: 2 T logits/s, which keeps up with 8 TB/s of fp32 ones.  The
 // odds that a sum's error moves a decision are its part of the distance
-// between two borders: at most 5.6e-11 for a draft, and 1e-5 even for a word
-// out of 100,000 equal ones if every error had the same sign.
-__device__ __forceinline__ double exp_neg(double x) {
+// between two borders: at most 5.6e-11 for a draft, and 5.6e-6 for a word out
+// of 100,000 equal ones even if every error had the same sign.
+__device__ __forceinline__ double exp64(double x) {
   constexpr double kShift = 6755399441055744.0;  // 1.5 * 2^52: n comes out in the sum's low bits
-  const double d = fmax(x, -760.0);
-  const double t = fma(d, 1.4426950408889634, kShift);
-  const double r = fma(t - kShift, -0.6931471805599453, d);
+  const double t = fma(x, 1.4426950408889634, kShift);
+  const double r = fma(t - kShift, -0.6931471805599453, x);
   double p = 0.00019907567086439808;
   p = fma(p, r, 0.0013948578255139586);
   p = fma(p, r, 0.00833328354312129);
@@ -94,84 +100,180 @@ __device__ __forceinline__ double exp_neg(double x) {
   p = fma(p, r, 1.0);
   return ldexp(p, (int)(uint32_t)__builtin_bit_cast(uint64_t, t));
 }
+constexpr double kNothing = -760.0;  // e^-760 is 0
+__device__ __forceinline__ double exp_rel(float z, float m) { return exp64(fmax((double)z - (double)m, kNothing)); }
+
+// ------------------------------------------------------- lane arithmetic
+
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// v of the lane that `ctrl` names (0 where there is none).
+template <int kCtrl, int kRows = 0xf>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, kCtrl, kRows, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), kCtrl, kRows, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, false));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;  // within 4, 4, 8, 16 lanes
+
+// Running sums over the wave's lanes, each lane's own included.
+__device__ __forceinline__ double wave_scan(double v) {
+  v += dpp<0x111>(v);  // the lane 1, 2, 4, 8 before, within 16
+  v += dpp<0x112>(v);
+  v += dpp<0x114>(v);
+  v += dpp<0x118>(v);
+  v += dpp<0x142, 0xa>(v);  // the last of the 16 before, to every second 16
+  v += dpp<0x143, 0xc>(v);  // the last of the first 32, to the others
+  return v;
+}
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum(double v) { return lane_value(wave_scan(v), 63); }
+// The lane before's (0 in the first).
+__device__ __forceinline__ double lane_before(double v) { return dpp<0x138>(v); }
 
 // maximum() returns NaN if either is (fmaxf does not).
 __device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float maximum16(float v) {  // of 16 lanes, in all of them
+  v = maximum(v, dpp<kXor1>(v));
+  v = maximum(v, dpp<kXor2>(v));
+  v = maximum(v, dpp<kMirror8>(v));
+  return maximum(v, dpp<kMirror16>(v));
+}
+__device__ __forceinline__ double sum16(double v) {
+  v += dpp<kXor1>(v);
+  v += dpp<kXor2>(v);
+  v += dpp<kMirror8>(v);
+  return v + dpp<kMirror16>(v);
+}
 __device__ __forceinline__ float wave_maximum(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = maximum(v, __shfl_xor(v, o, 64));
-  return v;
-}
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-// Inclusive running sums over the wave's lanes.
-__device__ __forceinline__ double wave_scan(double v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
-  return v;
+  v = maximum16(v);
+  v = maximum(v, __shfl_xor(v, 16, 64));
+  return maximum(v, __shfl_xor(v, 32, 64));
 }
 
-// Eight consecutive logits at z[i], those from n on as -infinity; any
-// alignment of the elements' own.  (The type is a branch here, the same for
-// the whole wave, and not a form of each kernel: their code would double, and
-// a block that runs once waits for its instructions as for its data.)
+// Eight consecutive logits of the row at z[row], from w0, or where those would
+// pass V the row's last eight; any alignment of the elements' own.  Returns
+// where they start: mask8 puts -infinity for those before w0.  With kShort
+// rows of less than eight words are met, of which a lane has one: each_lane()
+// words a lane.  (The type is a branch
+// here, the same for the whole wave, and not a form of each kernel: their code
+// would double, and a block that runs once waits for its instructions as for
+// its data.)
 typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
-__device__ __forceinline__ void load8(const void* z, int is16, int64_t i, int n, float (&x)[8]) {
-  if (n < 8) {
+__device__ __forceinline__ int each_lane(int V) { return V < 8 ? 1 : 8; }
+template <bool kShort>
+__device__ __forceinline__ int load8(const void* z, int is16, int64_t row, int w0, int V, float (&x)[8]) {
+  if (kShort && V < 8) {
+    x[0] = w0 < V ? logit(z, is16, row + w0) : -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = e < n ? logit(z, is16, i + e) : -INFINITY;
-  } else if (is16) {
-    const bf16x8u a = *(const bf16x8u*)((const __bf16*)z + i);
+    for (int e = 1; e < 8; ++e) x[e] = -INFINITY;
+    return w0;
+  }
+  const int at = min(w0, V - 8);
+  if (is16) {
+    const bf16x8u a = *(const bf16x8u*)((const __bf16*)z + row + at);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (float)a[e];
   } else {
-    const f32x4u a = *(const f32x4u*)((const float*)z + i), b = *(const f32x4u*)((const float*)z + i + 4);
+    const f32x4u* p = (const f32x4u*)((const float*)z + row + at);
+    const f32x4u a = p[0], b = p[1];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = e < 4 ? a[e] : b[e - 4];
+  }
+  return at;
+}
+__device__ __forceinline__ void mask8(int at, int w0, float (&x)[8]) {
+  if (at < w0) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = at + e < w0 ? -INFINITY : x[e];
   }
 }
 
 // ------------------------------------------------------------- row sums
 
-// The pair of one part of a row, by one wave: the n <= kPart logits at z.
-constexpr int kSteps = kPart / 512;  // eight logits a lane and step
-__device__ __forceinline__ RowSum part_sum(const void* z, int is16, int64_t at, int n) {
-  const int lane = threadIdx.x & 63;
-  float x[kSteps][8];
+// 2^(j / 32) into table[j], by any 32 threads.
+__device__ __forceinline__ void fill_table(double* table) {
+  if (threadIdx.x < 32) table[threadIdx.x] = exp2((double)threadIdx.x / 32);
+}
+// sum + e^x for x from -700 to 700: as exp64, but in steps of ln 2 / 32 and
+// with a polynomial of degree 3 (off by at most 9.9e-11 of e^x) that a factor
+// from the table makes good: 8 64-bit instructions with the addition, and 5
+// of 32 bits.  The table's 32 doubles lie in 64 banks, one bank's worth each, so
+// lanes never wait for each other.
+constexpr float kLowest = -700.f;
+__device__ __forceinline__ double add_exp(double sum, float x, const double* table) {
+  constexpr double kShift = 6755399441055744.0;
+  const double d = maximum(x, kLowest);
+  const double t = fma(d, 46.16624130844683, kShift);
+  const double r = fma(t - kShift, -0.02166084939249829, d);
+  const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+  const uint64_t b = __builtin_bit_cast(uint64_t, table[n & 31]);
+  uint32_t hi;  // (n / 32 on the exponent: the compiler would take a 64-bit addition for it)
+  asm("v_lshl_add_u32 %0, %1, 15, %2" : "=v"(hi) : "v"(n & ~31), "v"((uint32_t)(b >> 32)));
+  const double p = fma(fma(fma(0.16666804903930896, r, 0.5000040488943809), r, 0.9999999999525067), r, 1.0);
+  return fma(__builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)b), p, sum);
+}
+
+// The pair of up to kWavePart logits of a row, from word `from` to `to` or the
+// row's end, by one wave.  A largest of ordinary size is not taken off each
+// logit but divided out of their sum: its own term still counts exactly 1.
+constexpr float kPlain = 200.f;  // 2,048 e^200 and e^-200 are far inside a double's range
+constexpr int kSteps = kWavePart / 512;  // eight logits a lane and step
+template <bool kShort>
+__device__ __forceinline__ RowSum part_sum(const void* z, int is16, int64_t row, int from, int to, int V,
+                                           const double* table) {
+  const int w0 = from + (int)(threadIdx.x & 63) * (kShort ? each_lane(V) : 8);
+  float x[kSteps][8], m = -INFINITY;
+  int at[kSteps];
+  to = min(to, V);
   auto load = [&](int type) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) load8(z, type, at + i * 512 + lane * 8, n - (i * 512 + lane * 8), x[i]);
+    for (int i = 0; i < kSteps; ++i)
+      if (from + i * 512 < to) at[i] = load8<kShort>(z, type, row, w0 + i * 512, V, x[i]);
   };
   if (is16)
     load(1);
   else
     load(0);
-  float m = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i)
+  for (int i = 0; i < kSteps; ++i) {
+    if (from + i * 512 >= to) break;  // (a short part has few steps)
+    mask8(at[i], w0 + i * 512, x[i]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) m = maximum(m, x[i][e]);
+  }
   m = wave_maximum(m);
   double s = 0.0;
-  if (m > -INFINITY && m < INFINITY) {
+  if (m >= -kPlain && m <= kPlain) {
     double s1 = 0.0;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      if (i * 512 >= n) break;  // (a short row has few steps)
+      if (from + i * 512 >= to) break;
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        s += exp_neg((double)x[i][e] - (double)m);
-        s1 += exp_neg((double)x[i][e + 1] - (double)m);
+        s = add_exp(s, x[i][e], table);
+        s1 = add_exp(s1, x[i][e + 1], table);
       }
     }
-    s = wave_sum(s + s1);
+    s = wave_sum(s + s1) / add_exp(0.0, m, table);
+  } else if (m > -INFINITY && m < INFINITY) {
+#pragma unroll 1
+    for (int i = 0; from + i < to; i += 512) {
+      mask8(load8<kShort>(z, is16, row, w0 + i, V, x[0]), w0 + i, x[0]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += exp_rel(x[0][e], m);
+    }
+    s = wave_sum(s);
   }
   return RowSum{s, m};
 }
@@ -179,41 +281,39 @@ __device__ __forceinline__ RowSum part_sum(const void* z, int is16, int64_t at, 
 __device__ __forceinline__ RowSum merge(const RowSum& a, const RowSum& b) {
   const float m = maximum(a.m, b.m);
   if (!(m > -INFINITY && m < INFINITY)) return RowSum{0.0, m};
-  return RowSum{a.s * exp_neg((double)a.m - (double)m) + b.s * exp_neg((double)b.m - (double)m), m};
+  return RowSum{a.s * exp_rel(a.m, m) + b.s * exp_rel(b.m, m), m};
 }
 
-// A row's pair from its parts', by one wave.
-__device__ __forceinline__ RowSum merge_parts(const RowSum* r, int parts) {
-  const int lane = threadIdx.x & 63;
-  RowSum mine = lane < parts ? r[lane] : RowSum{0.0, -INFINITY};
-  for (int i = lane + 64; i < parts; i += 64) mine = merge(mine, r[i]);
-  const float m = wave_maximum(mine.m);
-  const bool ok = m > -INFINITY && m < INFINITY;
-  return RowSum{wave_sum(ok ? mine.s * exp_neg((double)mine.m - (double)m) : 0.0), m};
-}
-
-// One wave per part of a row.
-__global__ __launch_bounds__(kWaves * 64) void k_row_sums(VerifyArgs a, int64_t n_all) {
-  const int64_t id = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (id >= n_all) return;
-  const int64_t row = id / a.parts;
-  const int part = (int)(id % a.parts), n = min(kPart, a.V - part * kPart);
+// One block per part of a row.
+__global__ __launch_bounds__(kWaves * 64) void k_row_sums(VerifyArgs a) {
+  __shared__ RowSum sums[kWaves];
+  __shared__ double table[32];
+  fill_table(table);
+  __syncthreads();
+  const int64_t row = blockIdx.x / a.parts;
+  const int part = blockIdx.x % a.parts, wave = wave_index();
+  const int64_t thread = (int64_t)blockIdx.x * (kWaves * 64) + threadIdx.x;
+  if (thread < a.S) a.done[thread] = 0;  // (as many threads as sequences at least)
   const int64_t n_target = (int64_t)a.n_draft + a.S;
   const bool tgt = row < n_target;
-  const int64_t at = (tgt ? row * a.ld_t : (row - n_target) * a.ld_p) + (int64_t)part * kPart;
-  const RowSum r = part_sum(tgt ? a.target : a.proposal, tgt ? a.target16 : a.proposal16, at, n);
-  if ((threadIdx.x & 63) == 0) a.rows[id] = r;
+  const int from = part * a.part_len + wave * (a.part_len / kWaves);
+  const RowSum r = part_sum<false>(tgt ? a.target : a.proposal, tgt ? a.target16 : a.proposal16,
+                            tgt ? row * a.ld_t : (row - n_target) * a.ld_p, from, from + a.part_len / kWaves, a.V, table);
+  if ((threadIdx.x & 63) == 0) sums[wave] = r;
+  __syncthreads();
+  if (threadIdx.x == 0) a.rows[blockIdx.x] = merge(merge(sums[0], sums[1]), merge(sums[2], sums[3]));
 }
 
 // --------------------------------------------------------------- verdict
 
-// The verdict on sequence s, by a block of 2 kJudge waves: kJudge positions at
-// a time, a wave for each's target row and one for its proposal row
-// (row_sum(is_target, row)), then the first wave with a lane a position.  Log p
-// of each draft goes out too, and every position is looked at for it.  The
-// block's verdict is in *out after the call.
-template <class RowSumOf>
-__device__ __forceinline__ void judge(const VerifyArgs& a, int s, int o0, int o1, Verdict* out, RowSumOf&& row_sum) {
+// The verdict on sequence s by one block, kJudge positions at a time: fill(j0,
+// rows) leaves the sums of their target rows and proposal rows, then the first
+// wave takes a lane a position.  With write_logp log p of each draft goes out
+// too, and every position is looked at for it.  *out holds the verdict after
+// the call, for the whole block.
+template <class Fill>
+__device__ __forceinline__ void judge(const VerifyArgs& a, int s, int o0, int o1, bool write_logp, Verdict* out,
+                                      Fill&& fill) {
   __shared__ RowSum rows[2][kJudge];
   __shared__ int done;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -228,13 +328,7 @@ __device__ __forceinline__ void judge(const VerifyArgs& a, int s, int o0, int o1
   const int n = o1 - o0;
   if (threadIdx.x == 0) done = 0;
   for (int j0 = 0; j0 <= n; j0 += kJudge) {
-    const bool prop = wave >= kJudge;
-    const int jw = j0 + wave % kJudge;
-    if (jw < n + (prop ? 0 : 1) && (!prop || a.proposal)) {
-      const RowSum r = row_sum(!prop, prop ? (int64_t)o0 + jw : (int64_t)o0 + s + jw);
-      if (lane == 0) rows[prop][wave % kJudge] = r;
-    }
-    // what else a position is judged by, on its way meanwhile
+    // what else a position is judged by, on its way while the sums are made
     const int j = j0 + lane;
     const bool pos = wave == 0 && lane < kJudge && j <= n, has_p = pos && j < n && a.proposal;
     const int64_t tr = (int64_t)o0 + s + j, pr = (int64_t)o0 + j;
@@ -243,34 +337,27 @@ __device__ __forceinline__ void judge(const VerifyArgs& a, int s, int o0, int o1
     const bool d_ok = d >= 0 && d < a.V;
     const float zt = pos ? logit(a.target, a.target16, tr * a.ld_t + (d_ok ? d : 0)) : 0.f;
     const float zp = has_p ? logit(a.proposal, a.proposal16, pr * a.ld_p + (d_ok ? d : 0)) : 0.f;
+    fill(j0, n, rows);
     __syncthreads();
     if (wave == 0) {
       const RowSum rt = rows[0][lane % kJudge], rp = has_p ? rows[1][lane % kJudge] : RowSum{1.0, 0.f};
       const bool t_ok = is_distribution(rt);
       const int bad = !d_ok ? 1 : !t_ok || !is_distribution(rp) ? 2 : 0;
-      const double p = exp_neg((double)zt - (double)rt.m) / rt.s;
-      const double q = has_p ? exp_neg((double)zp - (double)rp.m) / rp.s : 1.0;
+      const double it = 1.0 / rt.s, ip = 1.0 / rp.s;
+      const double p = exp_rel(zt, rt.m) * it;
+      const double q = has_p ? exp_rel(zp, rp.m) * ip : 1.0;
       const bool end = pos && (j == n || bad || !((double)u * q < p));
       const uint64_t ends = __ballot(end);
       if (!done && ends && lane == __builtin_ctzll(ends)) {
-        *out = Verdict{rt, rp, tr, has_p ? pr : -1, j, bad, j < n && !a.proposal ? d : -1, 0};
+        *out = Verdict{tr, has_p ? pr : -1, it, ip, rt.m, rp.m, j, bad, j < n && !a.proposal ? d : -1, 0};
         done = 1;
       }
-      if (pos && j < n && a.draft_logp)
+      if (write_logp && pos && j < n)
         a.draft_logp[pr] = d_ok && t_ok ? (float)((double)zt - (double)rt.m - log(rt.s)) : __builtin_nanf("");
     }
     __syncthreads();
-    if (done && !a.draft_logp) break;
+    if (done && !write_logp) break;
   }
-}
-
-// One block a sequence.
-__global__ __launch_bounds__(2 * kJudge * 64) void k_judge(VerifyArgs a) {
-  const int s = blockIdx.x;
-  const int64_t n_target = (int64_t)a.n_draft + a.S;
-  judge(a, s, a.off[s], a.off[s + 1], a.verdict + s, [&](bool tgt, int64_t row) {
-    return merge_parts(a.rows + (tgt ? row : n_target + row) * a.parts, a.parts);
-  });
 }
 
 // A sequence that no word follows.
@@ -283,217 +370,272 @@ __device__ __forceinline__ void write_bad(const VerifyArgs& a, int s, const Verd
 
 // -------------------------------------------------------------- residual
 
-// What is left of words w0 .. w0 + 7 for the draw (nothing of those past V).
-__device__ __forceinline__ void residual8(const VerifyArgs& a, const Verdict& v, int w0, double (&r)[8]) {
-  float xt[8], xp[8];
-  const bool minus = v.p_row >= 0 && !v.whole;
-  load8(a.target, a.target16, v.t_row * a.ld_t + w0, a.V - w0, xt);
-  if (minus) load8(a.proposal, a.proposal16, v.p_row * a.ld_p + w0, a.V - w0, xp);
-  const double it = 1.0 / v.rt.s;
+// What is left of eight words for the draw: those from w0, or the last eight,
+// in which those before w0 count nothing.  `at` is where they start.
+struct Logits8 {
+  float t[8], p[8];
+  int at;
+};
+__device__ __forceinline__ bool minus_proposal(const Verdict& v) { return v.p_row >= 0 && !v.whole; }
+template <bool kShort>
+__device__ __forceinline__ void load_residual8(const VerifyArgs& a, const Verdict& v, int w0, Logits8& x) {
+  x.at = load8<kShort>(a.target, a.target16, v.t_row * a.ld_t, w0, a.V, x.t);
+  if (minus_proposal(v)) load8<kShort>(a.proposal, a.proposal16, v.p_row * a.ld_p, w0, a.V, x.p);
+}
+__device__ __forceinline__ void residual8(const Verdict& v, int w0, Logits8& x, double (&r)[8]) {
+  mask8(x.at, w0, x.t);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = exp_neg((double)xt[e] - (double)v.rt.m) * it;
-  if (minus) {
-    const double ip = 1.0 / v.rp.s;
+  for (int e = 0; e < 8; ++e) r[e] = exp_rel(x.t[e], v.mt) * v.it;
+  if (minus_proposal(v)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = fmax(r[e] - exp_neg((double)xp[e] - (double)v.rp.m) * ip, 0.0);
+    for (int e = 0; e < 8; ++e) r[e] = fmax(r[e] - exp_rel(x.p[e], v.mp) * v.ip, 0.0);
   } else if (v.cut >= 0 && !v.whole) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = w0 + e == v.cut ? 0.0 : r[e];
+    for (int e = 0; e < 8; ++e) r[e] = x.at + e == v.cut ? 0.0 : r[e];
   }
 }
 __device__ __forceinline__ double sum8(const double (&r)[8]) {
   return ((r[0] + r[1]) + (r[2] + r[3])) + ((r[4] + r[5]) + (r[6] + r[7]));
 }
 
-// The residual's sum over part p of the words, by one wave.
-__device__ __forceinline__ double rest_sum(const VerifyArgs& a, const Verdict& v, int part) {
-  double sum = 0.0;
-#pragma unroll 1
-  for (int i = 0; i < kRest / 512; ++i) {
-    double r[8];
-    residual8(a, v, part * kRest + i * 512 + (threadIdx.x & 63) * 8, r);
-    sum += sum8(r);
-  }
-  return wave_sum(sum);
-}
-
-// One wave per part of a sequence's words.
-__global__ __launch_bounds__(kWaves * 64) void k_residual(VerifyArgs a, int64_t n_all) {
-  const int64_t id = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (id >= n_all) return;
-  const int s = (int)(id / a.rests);
-  const Verdict v = a.verdict[s];
-  if (v.bad) return;
-  const double sum = rest_sum(a, v, (int)(id % a.rests));
-  if ((threadIdx.x & 63) == 0) a.rest[id] = sum;
-}
-
-// The first word of the block's (eight a thread from w0, whose residuals are
-// r and whose running sum starts at `run`) whose running sum passes the goal;
-// where rounding has left the goal at the whole sum, the last that has any.
-template <int NW>
-__device__ __forceinline__ int pick(const double (&r)[8], double run, double goal, int w0) {
-  __shared__ int word[NW], last[NW];
-  int hit_w = 0x7fffffff, last_w = -1;
+// The first of a lane's words (eight from `at`, residuals r, running sum before
+// them `run`) whose running sum passes the goal, and the last that has any.
+struct Picked {
+  int hit, last;
+};
+constexpr int kNone = 0x7fffffff;
+__device__ __forceinline__ Picked pick8(const double (&r)[8], double run, double goal, int at) {
+  Picked p{kNone, -1};
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     run += r[e];
     if (r[e] > 0.0) {
-      if (run > goal && hit_w == 0x7fffffff) hit_w = w0 + e;
-      last_w = w0 + e;
+      if (run > goal && p.hit == kNone) p.hit = at + e;
+      p.last = at + e;
     }
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    hit_w = min(hit_w, __shfl_xor(hit_w, o, 64));
-    last_w = max(last_w, __shfl_xor(last_w, o, 64));
-  }
-  const int wave = threadIdx.x >> 6;
-  if ((threadIdx.x & 63) == 0) {
-    word[wave] = hit_w;
-    last[wave] = last_w;
-  }
-  __syncthreads();
-  for (int i = 0; i < NW; ++i) {
-    hit_w = min(hit_w, word[i]);
-    last_w = max(last_w, last[i]);
-  }
-  return hit_w == 0x7fffffff ? last_w : hit_w;
+  return p;
 }
-
-// The sum of the block's values before this thread's, and all of them.
-template <int NW>
-__device__ __forceinline__ double block_before(double mine, double* total) {
-  __shared__ double sums[NW];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const double sc = wave_scan(mine), up = __shfl_up(sc, 1, 64);
-  __syncthreads();
-  if (lane == 63) sums[wave] = sc;
-  __syncthreads();
-  double before = 0.0, sum = 0.0;
-  for (int i = 0; i < NW; ++i) {
-    if (i == wave) before = sum;
-    sum += sums[i];
-  }
-  *total = sum;
-  return before + (lane > 0 ? up : 0.0);
+// The wave's.
+__device__ __forceinline__ Picked pick_wave(Picked p) {
+  const uint64_t hit = __ballot(p.hit != kNone), any = __ballot(p.last >= 0);
+  return Picked{hit ? __builtin_amdgcn_readlane(p.hit, __builtin_ctzll(hit)) : kNone,
+                any ? __builtin_amdgcn_readlane(p.last, 63 - __builtin_clzll(any)) : -1};
 }
 
 __device__ __forceinline__ void write_next(const VerifyArgs& a, int s, const Verdict& v, int w) {
   a.accepted[s] = v.kept;
   a.next[s] = w;
   if (a.next_logp)
-    a.next_logp[s] = (float)((double)logit(a.target, a.target16, v.t_row * a.ld_t + w) - (double)v.rt.m - log(v.rt.s));
+    a.next_logp[s] = (float)((double)logit(a.target, a.target16, v.t_row * a.ld_t + w) - (double)v.mt + log(v.it));
 }
 
-// The sequence's word from its residual's parts.  One block a sequence, eight
-// words of the part a thread.
-constexpr int kNextWaves = kRest / 512;
-__global__ __launch_bounds__(kNextWaves * 64) void k_next(VerifyArgs a) {
-  const int s = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Verdict v = a.verdict[s];
+// `blocks` blocks a sequence: the verdict, the residual over every blocks-th
+// 2,048 words, and by the last to finish the word.
+__global__ __launch_bounds__(kWaves * 64) void k_finish(VerifyArgs a, int blocks) {
+  __shared__ Verdict shared_v;
+  __shared__ int last_block;
+  const int s = blockIdx.x / blocks, b = blockIdx.x % blocks, lane = threadIdx.x & 63, wave = wave_index();
+  const int o0 = a.off[s], o1 = a.off[s + 1];
+  const float u = o1 >= 0 && o1 <= a.n_draft ? a.u[(int64_t)o1 + s] : 0.f;
+  judge(a, s, o0, o1, b == 0 && a.draft_logp, &shared_v, [&](int j0, int n, RowSum(&rows)[2][kJudge]) {
+    const int g = threadIdx.x >> 4, l16 = threadIdx.x & 15, j = j0 + g % kJudge;
+    const bool prop = g >= kJudge;
+    RowSum mine{0.0, -INFINITY};
+    if (j < n + (prop ? 0 : 1) && (!prop || a.proposal)) {
+      const int64_t row = prop ? (int64_t)a.n_draft + a.S + o0 + j : (int64_t)o0 + s + j;
+      for (int i = l16; i < a.parts; i += 16) {
+        const RowSum p = a.rows[row * a.parts + i];
+        mine = i < 16 ? p : merge(mine, p);
+      }
+    }
+    const float m = maximum16(mine.m);
+    const bool ok = m > -INFINITY && m < INFINITY;
+    const double sum = sum16(ok ? mine.s * exp_rel(mine.m, m) : 0.0);
+    if (l16 == 0) rows[prop][g % kJudge] = RowSum{sum, m};
+  });
+  Verdict v = shared_v;
   if (v.bad) {
-    if (threadIdx.x == 0) write_bad(a, s, v);
+    if (b == 0 && threadIdx.x == 0) write_bad(a, s, v);
     return;
   }
-  double* rest = a.rest + (int64_t)s * a.rests;
-  const double u = a.u[(int64_t)a.off[s + 1] + s];
-  auto running = [&](auto&& each) {  // each(part, its sum, the sum before it); returns the whole sum
+  double* rest = a.rest + (int64_t)s * a.units;
+  // units first, first + step, ..., the next one's logits on their way
+  auto sum_units = [&](int first, int step) {
+    Logits8 x, next;
+    for (int i = first, now = -1;; now = i, i += step, x = next) {
+      if (i < a.units) load_residual8<false>(a, v, i * kUnit + lane * 8, next);
+      if (now >= 0) {
+        double r[8];
+        residual8(v, now * kUnit + lane * 8, x, r);
+        const double sum = wave_sum(sum8(r));
+        if (lane == 0) __hip_atomic_store(rest + now, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      if (i >= a.units) break;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  // four consecutive units a lane; each(the first, their sums, the sum before them); returns the whole sum
+  auto running = [&](auto&& each) {
     double sum = 0.0;
-    for (int i = 0; i < a.rests; i += 64) {
-      const double x = i + lane < a.rests ? rest[i + lane] : 0.0;
-      const double sc = wave_scan(x);
-      const double up = __shfl_up(sc, 1, 64);
-      each(i, x, sum + (lane > 0 ? up : 0.0));
-      sum += __shfl(sc, 63, 64);
+    for (int i0 = 0; i0 < a.units; i0 += 256) {
+      double x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = i0 + lane * 4 + e < a.units
+                   ? __hip_atomic_load(rest + i0 + lane * 4 + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
+                   : 0.0;
+      const double scan = wave_scan((x[0] + x[1]) + (x[2] + x[3]));
+      each(i0 + lane * 4, x, sum + lane_before(scan));
+      sum += lane_value(scan, 63);
     }
     return sum;
   };
-  double total = running([](int, double, double) {});
-  if (!(total > 0.0)) {  // nothing left: p itself
-    v.whole = 1;
-    for (int p = wave; p < a.rests; p += kNextWaves) {
-      const double sum = rest_sum(a, v, p);
-      if (lane == 0) rest[p] = sum;
+  int first = b * kWaves + wave, step = blocks * kWaves;
+  double total;
+  for (;;) {
+    sum_units(first, step);
+    // The sums went past the XCD's cache and were waited for, so whoever counts
+    // this block among the finished ones finds them; a fence would write that
+    // whole cache back, block by block (64 sequences: 71 us in place of 20).
+    if (!v.whole) {
+      if (threadIdx.x == 0) last_block = atomicAdd(&a.done[s], 1u) == (uint32_t)blocks - 1;
+      __syncthreads();
+      if (!last_block) return;
     }
-    __syncthreads();
-    total = running([](int, double, double) {});
+    total = running([](int, const double(&)[4], double) {});
+    if (total > 0.0 || v.whole) break;
+    v.whole = 1;  // nothing left: p itself, by this block
+    first = wave;
+    step = kWaves;
   }
-  const double goal = u * total;
-  int part = -1, last_part = 0;
-  double before = 0.0, last_before = 0.0;
-  running([&](int i, double x, double ahead) {
-    const uint64_t hit = __ballot(x > 0.0 && ahead + x > goal), any = __ballot(x > 0.0);
-    if (part < 0 && hit) {
-      const int l = __builtin_ctzll(hit);
-      part = i + l;
-      before = __shfl(ahead, l, 64);
+  if (wave != 0) return;
+  // the first unit whose running sum passes the goal; where rounding has left
+  // the goal at the whole sum, the last that has any
+  const double goal = (double)u * total;
+  int unit = -1, last = 0;
+  double run = 0.0, last_run = 0.0;
+  running([&](int i, const double(&x)[4], double ahead) {
+    int hit = -1, any = -1;
+    double hit_run = 0.0, any_run = 0.0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (x[e] > 0.0) {
+        any = i + e;
+        any_run = ahead;
+        if (hit < 0 && ahead + x[e] > goal) {
+          hit = i + e;
+          hit_run = ahead;
+        }
+      }
+      ahead += x[e];
     }
-    if (any) {
-      const int l = 63 - __builtin_clzll(any);
-      last_part = i + l;
-      last_before = __shfl(ahead, l, 64);
+    const uint64_t hits = __ballot(hit >= 0), anys = __ballot(any >= 0);
+    if (unit < 0 && hits) {
+      unit = __builtin_amdgcn_readlane(hit, __builtin_ctzll(hits));
+      run = lane_value(hit_run, __builtin_ctzll(hits));
+    }
+    if (anys) {
+      last = __builtin_amdgcn_readlane(any, 63 - __builtin_clzll(anys));
+      last_run = lane_value(any_run, 63 - __builtin_clzll(anys));
     }
   });
-  if (part < 0) {  // (rounding can leave the goal at the whole sum)
-    part = last_part;
-    before = last_before;
+  if (unit < 0) {
+    unit = last;
+    run = last_run;
   }
-  const int w0 = part * kRest + (int)threadIdx.x * 8;
-  double r[8], all;
-  residual8(a, v, w0, r);
-  const double ahead = block_before<kNextWaves>(sum8(r), &all);
-  const int w = pick<kNextWaves>(r, before + ahead, goal, w0);
-  if (threadIdx.x == 0) write_next(a, s, v, w);
+  const int w0 = unit * kUnit + lane * 8;
+  double r[8];
+  Logits8 x;
+  load_residual8<false>(a, v, w0, x);
+  residual8(v, w0, x, r);
+  const double scan = wave_scan(sum8(r));
+  const Picked p = pick_wave(pick8(r, run + lane_before(scan), goal, x.at));
+  if (lane == 0) write_next(a, s, v, p.hit != kNone ? p.hit : p.last);
 }
 
 // ------------------------------------------------------- small vocabularies
 
 // A sequence by one block: V <= kSmallV.
 __global__ __launch_bounds__(2 * kJudge * 64) void k_verify_small(VerifyArgs a) {
+  constexpr int W = 2 * kJudge;
   __shared__ Verdict shared_v;
-  const int s = blockIdx.x, o0 = a.off[s], o1 = a.off[s + 1];
-  judge(a, s, o0, o1, &shared_v, [&](bool tgt, int64_t row) {
-    const void* z = tgt ? a.target : a.proposal;
-    const int is16 = tgt ? a.target16 : a.proposal16;
-    const int64_t at = row * (tgt ? a.ld_t : a.ld_p);
+  __shared__ double sums[2][W];
+  __shared__ Picked picks[W];
+  __shared__ double table[32];
+  fill_table(table);
+  __syncthreads();
+  const int s = blockIdx.x, o0 = a.off[s], o1 = a.off[s + 1], lane = threadIdx.x & 63, wave = wave_index();
+  const float u = o1 >= 0 && o1 <= a.n_draft ? a.u[(int64_t)o1 + s] : 0.f;
+  judge(a, s, o0, o1, a.draft_logp != nullptr, &shared_v, [&](int j0, int n, RowSum(&rows)[2][kJudge]) {
+    const bool prop = wave >= kJudge;
+    const int j = j0 + wave % kJudge;
+    if (j >= n + (prop ? 0 : 1) || (prop && !a.proposal)) return;
+    const void* z = prop ? a.proposal : a.target;
+    const int is16 = prop ? a.proposal16 : a.target16;
+    const int64_t at = prop ? ((int64_t)o0 + j) * a.ld_p : ((int64_t)o0 + s + j) * a.ld_t;
     RowSum r{0.0, -INFINITY};
 #pragma unroll 1
-    for (int i = 0; i < a.V; i += kPart) {
-      const RowSum p = part_sum(z, is16, at + i, min(kPart, a.V - i));
+    for (int i = 0; i < a.V; i += kWavePart) {
+      const RowSum p = part_sum<true>(z, is16, at, i, i + kWavePart, a.V, table);
       r = i ? merge(r, p) : p;
     }
-    return r;
+    if (lane == 0) rows[prop][wave % kJudge] = r;
   });
   Verdict v = shared_v;
   if (v.bad) {
     if (threadIdx.x == 0) write_bad(a, s, v);
     return;
   }
-  const int w0 = (int)threadIdx.x * 8;
-  double r[8], total, ahead;
-  residual8(a, v, w0, r);
-  ahead = block_before<2 * kJudge>(sum8(r), &total);
-  if (!(total > 0.0)) {  // nothing left: p itself
-    v.whole = 1;
-    residual8(a, v, w0, r);
-    ahead = block_before<2 * kJudge>(sum8(r), &total);
+  const int w0 = (int)threadIdx.x * each_lane(a.V);
+  Logits8 x;
+  double r[8], total = 0.0, run = 0.0;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {  // (a second one where nothing is left: p itself)
+    v.whole = pass;
+    if (wave == 0 || wave * 512 < a.V) {
+      load_residual8<true>(a, v, w0, x);
+      residual8(v, w0, x, r);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e] = 0.0;
+    }
+    const double scan = wave_scan(sum8(r));
+    if (lane == 63) sums[pass][wave] = scan;
+    __syncthreads();
+    total = run = 0.0;
+    for (int i = 0; i < W; ++i) {
+      if (i == wave) run = total;
+      total += sums[pass][i];
+    }
+    run += lane_before(scan);
+    if (total > 0.0) break;
   }
-  const int w = pick<2 * kJudge>(r, ahead, (double)a.u[(int64_t)o1 + s] * total, w0);
-  if (threadIdx.x == 0) write_next(a, s, v, w);
+  const Picked mine = pick_wave(pick8(r, run, (double)u * total, x.at));
+  if (lane == 0) picks[wave] = mine;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int hit = kNone, last = -1;
+    for (int i = 0; i < W; ++i) {
+      hit = min(hit, picks[i].hit);
+      last = max(last, picks[i].last);
+    }
+    write_next(a, s, v, hit != kNone ? hit : last);
+  }
 }
 
 // Workspace layout (offsets in bytes, 256-aligned).
+constexpr int kLeastPart = kWaves * 512;  // a row's parts are no shorter than this
 struct VerifyWs {
-  size_t rows, verdict, rest, total;
+  size_t rows, rest, done, total;
 };
 VerifyWs verify_ws(int V, int64_t S, int64_t n_draft) {
-  const size_t parts = (size_t)ceil_div(V, kPart), rests = (size_t)ceil_div(V, kRest);
+  const size_t parts = (size_t)ceil_div(V, kLeastPart), units = (size_t)ceil_div(V, kUnit);
   auto al = [](size_t x) { return (x + 255) / 256 * 256; };
   VerifyWs L{};
-  L.verdict = L.rows + al((size_t)(S + 2 * n_draft) * parts * sizeof(RowSum));
-  L.rest = L.verdict + al((size_t)S * sizeof(Verdict));
-  L.total = L.rest + al((size_t)S * rests * sizeof(double));
+  L.rest = L.rows + al((size_t)(S + 2 * n_draft) * parts * sizeof(RowSum));
+  L.done = L.rest + al((size_t)S * units * sizeof(double));
+  L.total = L.done + al((size_t)S * sizeof(uint32_t));
   return L;
 }
 
@@ -524,11 +666,15 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   if (((uintptr_t)d_target & (target_type == NMT_BF16 ? 1 : 3)) ||
       ((uintptr_t)d_proposal & (proposal_type == NMT_BF16 ? 1 : 3)))
     return entry_fail(NMT_EINVAL, "logits must be aligned to their elements");
-  const int parts = ceil_div(V, kPart), rests = ceil_div(V, kRest);
-  const int64_t n_rows = (int64_t)n_draft + S + (d_proposal ? n_draft : 0), n_parts = n_rows * parts;
-  const int64_t n_rests = (int64_t)S * rests;
-  auto blocks = [](int64_t waves) { return (waves + kWaves - 1) / kWaves; };
-  if (blocks(n_parts) > 0x7fffffff || blocks(n_rests) > 0x7fffffff)
+  // Parts as long as the grid still gives each CU four blocks, and blocks of a
+  // sequence's residual until every wave has one unit or each CU eight.
+  const int64_t n_rows = (int64_t)n_draft + S + (d_proposal ? n_draft : 0);
+  int part_len = kWaves * kWavePart;
+  while (part_len > kLeastPart && n_rows * ceil_div(V, part_len) < 4 * kCUs) part_len /= 2;
+  const int parts = ceil_div(V, part_len), units = ceil_div(V, kUnit);
+  const int64_t n_parts = n_rows * parts;
+  const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, kWaves), 4 * kCUs / S));
+  if (n_parts > 0x7fffffff || (int64_t)S * blocks > 0x7fffffff)
     return entry_fail(NMT_EINVAL, "too many rows of logits for one call");
   const VerifyWs L = verify_ws(V, S, n_draft);
   if (!d_workspace || ((uintptr_t)d_workspace & 255)) return entry_fail(NMT_EINVAL, "workspace must be 256-byte aligned");
@@ -536,10 +682,10 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   const nmt_status rc = entry_check_device(m);
   if (rc != NMT_OK) return rc;
   char* ws = (char*)d_workspace;
-  const VerifyArgs a{S, n_draft, V, parts, rests, d_draft_off, d_draft, d_target, d_proposal, target_type == NMT_BF16,
-                     proposal_type == NMT_BF16, ld_target, ld_proposal, d_u, d_accepted, d_next, d_draft_logp,
-                     d_next_logp, (RowSum*)(ws + L.rows), (Verdict*)(ws + L.verdict), (double*)(ws + L.rest),
-                     error_flag(m)};
+  const VerifyArgs a{S, n_draft, V, parts, part_len, units, d_draft_off, d_draft, d_target, d_proposal,
+                     target_type == NMT_BF16, proposal_type == NMT_BF16, ld_target, ld_proposal, d_u, d_accepted,
+                     d_next, d_draft_logp, d_next_logp, (RowSum*)(ws + L.rows), (double*)(ws + L.rest),
+                     (uint32_t*)(ws + L.done), error_flag(m)};
   hipStream_t st = (hipStream_t)stream;
   hipError_t e = hipSuccess;
   auto run = [&](auto* kernel, int64_t grid, int threads, auto... args) {
@@ -550,10 +696,8 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   if (V <= kSmallV) {
     run(k_verify_small, S, 2 * kJudge * 64);
   } else {
-    run(k_row_sums, blocks(n_parts), kWaves * 64, n_parts);
-    run(k_judge, S, 2 * kJudge * 64);
-    run(k_residual, blocks(n_rests), kWaves * 64, n_rests);
-    run(k_next, S, kNextWaves * 64);
+    run(k_row_sums, n_parts, kWaves * 64);
+    run(k_finish, (int64_t)S * blocks, kWaves * 64, blocks);
   }
   if (e != hipSuccess) return entry_hip_fail(e, "nmt_verify_drafts");
   return entry_ok();
