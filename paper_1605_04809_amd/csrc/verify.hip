@@ -201,13 +201,15 @@ __device__ __forceinline__ void mask8(int at, int w0, float (&x)[8]) {
 
 // ------------------------------------------------------------- row sums
 
-// 2^(j / 32) into table[j], by any 32 threads.
+// 2^(j / 32) into table[j], less j << 15 in the upper half: n << 15 on that
+// puts n / 32 on the exponent, whole steps alone.
 __device__ __forceinline__ void fill_table(double* table) {
-  if (threadIdx.x < 32) table[threadIdx.x] = exp2((double)threadIdx.x / 32);
+  const uint64_t j = threadIdx.x;
+  if (j < 32) table[j] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, exp2((double)j / 32)) - (j << 47));
 }
 // sum + e^x for x from -700 to 700: as exp64, but in steps of ln 2 / 32 and
 // with a polynomial of degree 3 (off by at most 9.9e-11 of e^x) that a factor
-// from the table makes good: 8 64-bit instructions with the addition, and 5
+// from the table makes good: 8 64-bit instructions with the addition, and 4
 // of 32 bits.  The table's 32 doubles lie in 64 banks, one bank's worth each, so
 // lanes never wait for each other.
 constexpr float kLowest = -700.f;
@@ -218,8 +220,8 @@ __device__ __forceinline__ double add_exp(double sum, float x, const double* tab
   const double r = fma(t - kShift, -0.02166084939249829, d);
   const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
   const uint64_t b = __builtin_bit_cast(uint64_t, table[n & 31]);
-  uint32_t hi;  // (n / 32 on the exponent: the compiler would take a 64-bit addition for it)
-  asm("v_lshl_add_u32 %0, %1, 15, %2" : "=v"(hi) : "v"(n & ~31), "v"((uint32_t)(b >> 32)));
+  uint32_t hi;  // (the compiler would take a 64-bit addition for it)
+  asm("v_lshl_add_u32 %0, %1, 15, %2" : "=v"(hi) : "v"(n), "v"((uint32_t)(b >> 32)));
   const double p = fma(fma(fma(0.16666804903930896, r, 0.5000040488943809), r, 0.9999999999525067), r, 1.0);
   return fma(__builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)b), p, sum);
 }
