@@ -668,8 +668,10 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   if (((uintptr_t)d_target & (target_type == NMT_BF16 ? 1 : 3)) ||
       ((uintptr_t)d_proposal & (proposal_type == NMT_BF16 ? 1 : 3)))
     return entry_fail(NMT_EINVAL, "logits must be aligned to their elements");
-  // Parts as long as the grid still gives each CU four blocks, and blocks of a
-  // sequence's residual until every wave has one unit or each CU eight.
+  // Parts as long as the grid still gives each CU four blocks (parts four times
+  // as long measured the same), and blocks of a sequence's residual until every
+  // wave has one unit or each CU four blocks, each of which judges its sequence
+  // by itself (64 sequences of 50,000 words: 45 us a call with eight, 41 with four).
   const int64_t n_rows = (int64_t)n_draft + S + (d_proposal ? n_draft : 0);
   int part_len = kWaves * kWavePart;
   while (part_len > kLeastPart && n_rows * ceil_div(V, part_len) < 4 * kCUs) part_len /= 2;

@@ -287,28 +287,26 @@ __global__ __launch_bounds__(w4_waves(RM) * 64) __attribute__((amdgpu_waves_per_
 
   // a K block's codes, scales and zero points, as they are in memory
   typedef ST scales_t __attribute__((ext_vector_type(GPB)));
+  using zeros_t = std::conditional_t<GPB == 4, uint32_t, std::conditional_t<GPB == 2, uint16_t, uint8_t>>;
   struct Block {
     uint4 code;
     scales_t scale;
-    uint32_t zero;
+    zeros_t zero;
   };
+  // Loads without a branch, or the compiler cannot tell how many are under way
+  // and waits for all: past the end the last block is read once more, and
+  // without zero points, in their place, bytes of the scales.
+  const zeros_t* zeros = (const zeros_t*)(a.zeros ? (const void*)a.zeros : a.scales);
   auto load = [&](Block& b, int tile, int kb) {
-    if (tile >= a.tiles || kb >= a.kblocks) return;
-    const int64_t tb = (int64_t)tile * a.kblocks + kb;
+    const int64_t tb = (int64_t)min(tile, a.tiles - 1) * a.kblocks + min(kb, a.kblocks - 1);
     b.code = (a.codes + tb * 64)[lane];
     b.scale = ((const scales_t*)a.scales + tb * kW4Cols)[r16];
-    b.zero = 0x08080808u;
-    if (a.zeros) {
-      if constexpr (GPB == 4)
-        b.zero = ((const uint32_t*)a.zeros + tb * kW4Cols)[r16];
-      else if constexpr (GPB == 2)
-        b.zero = ((const uint16_t*)a.zeros + tb * kW4Cols)[r16];
-      else
-        b.zero = (a.zeros + tb * kW4Cols)[r16];
-    }
+    b.zero = (zeros + tb * kW4Cols)[r16];
   };
+  // tiles go round the strips, then their waves: what is left in the last round
+  // falls on one wave of many CUs, not on all of a few
   const int tile_step = sh.strips * per_block;
-  int tile = strip * per_block + wave / sh.wk;
+  int tile = strip + wave / sh.wk * sh.strips;
   Block ring[D];
 #pragma unroll
   for (int d = 0; d < D; ++d) load(ring[d], tile, d * sh.wk + wk);
@@ -393,6 +391,7 @@ __global__ __launch_bounds__(w4_waves(RM) * 64) __attribute__((amdgpu_waves_per_
 #pragma unroll
         for (int z = 0; z < HV; ++z) xf[s & 1][i][z] = (from + x_row[s])[(s * HV + z) * 4 * RM + i * 16];
     };
+    const uint32_t zeros4 = a.zeros ? (uint32_t)b.zero : 0x08080808u;
     fetch(0);
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -401,7 +400,7 @@ __global__ __launch_bounds__(w4_waves(RM) * 64) __attribute__((amdgpu_waves_per_
       const int g = s / kStepsPerGroup;
       if (s < 3) fetch(s + 1);
       // the group's zero point in both halves; -(1024 + z) and -(64 + z) as bits
-      const uint32_t z = __builtin_amdgcn_perm(0u, b.zero, 0x0c000c00u | (uint32_t)g * 0x00010001u);
+      const uint32_t z = __builtin_amdgcn_perm(0u, zeros4, 0x0c000c00u | (uint32_t)g * 0x00010001u);
       const f16x2 zl = __builtin_bit_cast(f16x2, z | 0xe400e400u);
       const f16x2 zh = __builtin_bit_cast(f16x2, (z << 4) | 0xd400d400u);
       const uint32_t w = s == 0 ? b.code.x : s == 1 ? b.code.y : s == 2 ? b.code.z : b.code.w;
@@ -429,7 +428,7 @@ __global__ __launch_bounds__(w4_waves(RM) * 64) __attribute__((amdgpu_waves_per_
 
   f32x4* red = lds + sh.chunk * (16 * HV * RM + 4 * RT) + wave * (RT * 64) + lane;
   // every wave goes round as often as the block's first has tiles
-  for (int first = strip * per_block; first < a.tiles; first += tile_step, tile += tile_step) {
+  for (int first = strip; first < a.tiles; first += tile_step, tile += tile_step) {
     const float bias = a.bias && tile < a.tiles ? a.bias[tile * kW4Cols + r16] : 0.f;
 #pragma unroll
     for (int i = 0; i < RT; ++i) sum[i] = zero4();
@@ -516,9 +515,9 @@ hipError_t launch_product(const W4Args& a, bool x16, bool s16, int gpb, int cus,
     sh.wk *= 2;
   const int step = depth * sh.wk;
   sh.chunk = most >= a.kblocks ? a.kblocks : most / step * step;
-  // as many blocks as run at once, evenly loaded
-  const int want = ceil_div(a.tiles, W / sh.wk), fit = std::max(1, per_cu * cus / sh.row_blocks);
-  sh.strips = (int)round_up(ceil_div(want, ceil_div(want, fit)), 8);
+  // as many blocks as run at once
+  const int want = ceil_div(a.tiles, W / sh.wk), fit = per_cu * cus / sh.row_blocks;
+  sh.strips = want <= fit ? (int)round_up(want, 8) : std::max(fit / 8 * 8, 8);
   auto types = [&](auto rm, auto g) {
     constexpr int R = decltype(rm)::value, G = decltype(g)::value;
     return x16 ? (s16 ? launch_form<R, G, true, true>(a, sh, st) : launch_form<R, G, true, false>(a, sh, st))
