@@ -389,8 +389,13 @@ __device__ __forceinline__ void residual8(const Verdict& v, int w0, Logits8& x, 
 #pragma unroll
   for (int e = 0; e < 8; ++e) r[e] = exp_rel(x.t[e], v.mt) * v.it;
   if (minus_proposal(v)) {
+    // (both products rounded, and not one inside a multiply-add: equal rows leave nothing)
+#pragma clang fp contract(off)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = fmax(r[e] - exp_rel(x.p[e], v.mp) * v.ip, 0.0);
+    for (int e = 0; e < 8; ++e) {
+      const double q = exp_rel(x.p[e], v.mp) * v.ip;
+      r[e] = fmax(r[e] - q, 0.0);
+    }
   } else if (v.cut >= 0 && !v.whole) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) r[e] = x.at + e == v.cut ? 0.0 : r[e];

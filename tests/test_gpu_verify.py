@@ -308,3 +308,176 @@ def test_streams_graphs_and_a_used_workspace(V, S, k):
         check()
     assert nb.nmt_stream_status(model) == nb.NMT_OK
     model.close()
+
+
+# ---- vocabularies of more than 8,192 words: two launches, a row in parts, a
+# residual in units of 512 words
+
+@pytest.mark.parametrize("V", [8191, 8192, 8193, 8199, 8200, 10240, 16385, 131072, 131073, 300001])
+@pytest.mark.parametrize("tt,pt", [("float32", "float32"), ("bfloat16", "bfloat16")])
+def test_borders_of_parts_and_units(V, tt, pt):
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    model = _model(nb, V)
+    off, draft, target, prop, u = _inputs(np.random.default_rng(V), V, 5, 3, tt == "bfloat16", pt == "bfloat16")
+    # the row's last words carry some of the sums, and the largest u draws one of them
+    target[:, -9:] += 4.0
+    target = dc.round_bf16(target) if tt == "bfloat16" else target
+    u[off[1:] + np.arange(5)] = np.float32([0.0, 0.25, 0.999, 1.0 - 2.0 ** -24, 0.5])
+    ins = (off, draft, target, prop, u)
+    _same(_run(torch, nb, model, *ins, tt=tt, pt=pt), dc.verify(*ins), target)
+    assert nb.nmt_stream_status(model) == nb.NMT_OK
+    model.close()
+
+
+@pytest.mark.parametrize("S,k,certain", [(2, 40, False), (2, 40, True), (1500, 1, False), (1100, 0, True)])
+def test_long_drafts_and_many_sequences(S, k, certain):
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    V = 8300
+    model = _model(nb, V)
+    ins = _inputs(np.random.default_rng(S + k), V, S, k, certain=certain, spread=4.0, near=0.3)
+    want = dc.verify(*ins)
+    _same(_run(torch, nb, model, *ins), want, ins[2])
+    d = [_dev(torch, a) if a is not None else None for a in ins]
+    acc, nxt = (torch.zeros(S, dtype=torch.int32, device="cuda") for _ in range(2))
+    nb.nmt_verify_drafts(model, *d, acc, nxt)     # without log p: no position behind the end is looked at
+    np.testing.assert_array_equal(acc.cpu().numpy(), want[0])
+    np.testing.assert_array_equal(nxt.cpu().numpy(), want[1])
+    model.close()
+
+
+@pytest.mark.parametrize("tt,pt", [("float32", "bfloat16"), ("bfloat16", "float32")])
+@pytest.mark.parametrize("pad,shift,V", [(8, 0, 9000), (5, 3, 9000), (1, 1, 9001), (0, 7, 12289)])
+def test_types_strides_and_alignment_of_long_rows(tt, pt, pad, shift, V):
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    model = _model(nb, V)
+    ins = _inputs(np.random.default_rng(pad + V), V, 6, 4, tt == "bfloat16", pt == "bfloat16")
+    got = _run(torch, nb, model, *ins, tt=tt, pt=pt, pad=pad, shift=shift)
+    _same(got, dc.verify(*ins), ins[2])
+    model.close()
+
+
+@pytest.mark.parametrize("mask", [0.3, 0.9995])
+def test_masked_words_of_long_rows(mask):
+    """Whole parts and units of nothing but -infinity; the type's lowest value."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    V = 20000
+    model = _model(nb, V)
+    rng = np.random.default_rng(V)
+    off, draft, target, prop, u = _inputs(rng, V, 12, 4, mask=mask)
+    low = target.copy()
+    low[np.isneginf(low)] = np.finfo(np.float32).min
+    other = draft.copy()
+    other[::3] = rng.integers(0, V, size=len(other[::3]))
+    for d, t in ((draft, target), (other, target), (draft, low)):
+        ins = (off, d, t, prop, u)
+        _same(_run(torch, nb, model, *ins), dc.verify(*ins), t)
+    assert nb.nmt_stream_status(model) == nb.NMT_OK
+    model.close()
+
+
+@pytest.mark.parametrize("V", [1500, 20000])
+@pytest.mark.parametrize("spread,shift", [(0.0, 0.0), (0.0, 5e4), (1.0, 199.0), (1.0, 201.0), (1.0, -199.0), (1.0, -201.0),
+                                          (1.0, -690.0), (300.0, 0.0), (3e4, 0.0), (1e38, 0.0)])
+def test_rows_of_any_size(V, spread, shift):
+    """Logits far from 0, whose largest is taken off before the exponential,
+    beside parts of ordinary ones."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    model = _model(nb, V)
+    rng = np.random.default_rng(3)
+    off, draft, target, prop, u = _inputs(rng, V, 8, 3, spread=1.0)
+    target = (np.float32(spread) * np.clip(target, -3, 3) + np.float32(shift)).astype(np.float32)
+    prop = (np.float32(spread) * np.clip(prop, -3, 3) + np.float32(shift)).astype(np.float32)
+    target[::2, : V // 2] = np.clip(target[::2, : V // 2], -50, 50)
+    ins = (off, draft, target, prop, u)
+    _same(_run(torch, nb, model, *ins), dc.verify(*ins), target)
+    assert nb.nmt_stream_status(model) == nb.NMT_OK
+    model.close()
+
+
+@pytest.mark.parametrize("V", [900, 9000, 140000])
+def test_nothing_left_of_a_long_row(V):
+    """Target and proposal alike, and a draft that neither gives: p itself; a
+    target of one word, certain drafts: p without the draft is nothing."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    model = _model(nb, V)
+    rng = np.random.default_rng(7)
+    z = rng.standard_normal((2, V)).astype(np.float32)
+    z[0, [3, V - 1]] = -np.inf
+    for d, u in ((3, 0.3), (V - 1, 0.0), (V - 1, 1.0 - 2.0 ** -24), (3, 0.999)):
+        ins = ([0, 1], [d], z, z[:1], np.array([0.0, u], np.float32))
+        got = _run(torch, nb, model, *ins)
+        assert got[0][0] == 0 and got[1][0] not in (-1, 3, V - 1)
+        _same(got, dc.verify(*ins), z)
+    one = np.full((2, V), -np.inf, np.float32)
+    one[:, V - 2] = 3.0
+    for d, u0 in ((V - 2, 0.5), (5, 0.5)):
+        ins = ([0, 1], [d], one, None, np.array([u0, 0.7], np.float32))
+        got = _run(torch, nb, model, *ins)
+        assert (got[0][0], got[1][0]) == ((1, V - 2) if d == V - 2 else (0, V - 2))
+        _same(got, dc.verify(*ins), one)
+    assert nb.nmt_stream_status(model) == nb.NMT_OK
+    model.close()
+
+
+def test_bad_long_rows_are_flagged_and_stay_alone():
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    V, S = 9001, 6
+    model = _model(nb, V)
+    rng = np.random.default_rng(4)
+    off = (2 * np.arange(S + 1)).astype(np.int32)
+    nd = int(off[-1])
+    target = rng.standard_normal((nd + S, V)).astype(np.float32)
+    prop = rng.standard_normal((nd, V)).astype(np.float32)
+    draft = rng.integers(0, V, size=nd).astype(np.int32)
+    u = np.zeros(nd + S, np.float32)
+    u[off[1:] + np.arange(S)] = 0.5
+    clean = dc.verify(off, draft, target, prop, u)
+    bad, d2, p2 = target.copy(), draft.copy(), prop.copy()
+    bad[off[1] + 1 + 1, V - 1] = np.nan     # sequence 1, position 1
+    bad[off[2] + 2 + 2] = -np.inf           # sequence 2, the row behind its drafts
+    d2[off[3]] = V                          # sequence 3, position 0
+    p2[off[4] + 1, 8500] = np.inf           # sequence 4, position 1
+    got = _run(torch, nb, model, off, d2, bad, p2, u)
+    assert nb.nmt_stream_status(model) == nb.NMT_ERANGE
+    for s, kept in ((1, 1), (2, 2), (3, 0), (4, 1)):
+        assert (got[0][s], got[1][s]) == (kept, -1) and np.isnan(got[3][s]), s
+    for s in (0, 5):
+        assert (got[0][s], got[1][s]) == (clean[0][s], clean[1][s])
+    for off_bad in ([0, 2, 1, 3], [0, -1, 2, 3], [0, 1, 2, 9], [-2, 1, 2, 3]):
+        out = _run(torch, nb, model, off_bad, draft[:3], target[:6], prop[:3], u[:6])
+        assert nb.nmt_stream_status(model) == nb.NMT_ERANGE
+        for s in range(3):
+            if not 0 <= off_bad[s] <= off_bad[s + 1] <= 3:
+                assert (out[0][s], out[1][s]) == (0, -1)
+    model.close()
+
+
+def test_two_calls_at_once():
+    """On two streams, a workspace each, many times over."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    V, S = 20000, 30
+    model = _model(nb, V)
+    jobs = []
+    for seed in (1, 2):
+        ins = _inputs(np.random.default_rng(seed), V, S, 3)
+        acc, nxt = (torch.zeros(S, dtype=torch.int32, device="cuda") for _ in range(2))
+        jobs.append((dc.verify(*ins), [_dev(torch, a) for a in ins], acc, nxt, torch.cuda.Stream(),
+                     torch.empty(nb.nmt_verify_workspace_bytes(model, S, len(ins[1])), dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for _, d, acc, nxt, stream, ws in jobs:
+            with torch.cuda.stream(stream):
+                nb.nmt_verify_drafts(model, *d, acc, nxt, workspace=ws)
+    torch.cuda.synchronize()
+    for want, _, acc, nxt, _, _ in jobs:
+        np.testing.assert_array_equal(acc.cpu().numpy(), want[0])
+        np.testing.assert_array_equal(nxt.cpu().numpy(), want[1])
+    model.close()

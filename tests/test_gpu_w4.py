@@ -297,3 +297,53 @@ def test_a_row_does_not_depend_on_the_others():
         out.append(y.cpu().numpy()[[0, 33, 69]])
     np.testing.assert_array_equal(out[0], out[1])
     w.close()
+
+
+@pytest.mark.parametrize("K,N,M,group", [(500, 200, 3, 96), (500, 200, 40, 160), (1001, 100, 20, 192), (700, 50, 1, 320),
+                                         (96, 48, 2, 96), (4096, 64, 5, 4096), (500, 33, 17, 992)])
+def test_groups_that_do_not_divide_a_block(K, N, M, group):
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    _check(torch, nb, K, N, M, group, True, True, "f32", "f32", "bf16", seed=group)
+
+
+@pytest.mark.parametrize("K,N,M,xt", [(6001, 500, 5, "f32"), (6001, 500, 16, "f32"), (6001, 500, 17, "f32"),
+                                      (6001, 500, 48, "f32"), (6001, 9000, 12, "f32"), (6001, 9000, 40, "bf16"),
+                                      (3500, 34000, 33, "f32"), (3500, 17000, 64, "f32"), (12000, 20, 1, "bf16"),
+                                      (1500, 66000, 20, "f32")])
+@pytest.mark.parametrize("group", [32, 128])
+def test_long_columns(K, N, M, xt, group):
+    """K in chunks, split between waves, over several rounds of columns."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    _check(torch, nb, K, N, M, group, True, True, xt, "f32", "f32", seed=K + M)
+
+
+@pytest.mark.parametrize("M", [2, 4, 5, 8, 15, 16, 17, 31, 32, 33, 47, 48, 49, 63, 64, 80, 81, 97])
+@pytest.mark.parametrize("N", [2000, 40000])
+def test_rows(M, N):
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    _check(torch, nb, 260, N, M, 64, True, True, "f32", "bf16", "bf16", seed=M)
+
+
+def test_two_products_at_once():
+    """One matrix on two streams: a product holds nothing between calls."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    rng = np.random.default_rng(5)
+    c = dc.make_w4(rng, 500, 5000, 64, True, True)
+    w = _handle(nb, c, 500, 5000, 64)
+    xs = [torch.from_numpy(rng.standard_normal((M, 500)).astype(np.float32)).cuda() for M in (3, 40)]
+    want = [torch.zeros((len(x), 5000), device="cuda") for x in xs]
+    for x, y in zip(xs, want):
+        nb.nmt_w4_product(w, x, y)
+    torch.cuda.synchronize()
+    got, streams = [torch.zeros_like(y) for y in want], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        for x, y, s in zip(xs, got, streams):
+            with torch.cuda.stream(s):
+                nb.nmt_w4_product(w, x, y)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    w.close()
