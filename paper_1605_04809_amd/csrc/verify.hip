@@ -683,7 +683,8 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   const int parts = ceil_div(V, part_len), units = ceil_div(V, kUnit);
   const int64_t n_parts = n_rows * parts;
   const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, kWaves), 4 * kCUs / S));
-  if (n_parts > 0x7fffffff || (int64_t)S * blocks > 0x7fffffff)
+  // a launch's threads are counted in 32 bits
+  if (V <= kSmallV ? S >= (1 << 22) : std::max(n_parts, (int64_t)S * blocks) >= (1 << 24))
     return entry_fail(NMT_EINVAL, "too many rows of logits for one call");
   const VerifyWs L = verify_ws(V, S, n_draft);
   if (!d_workspace || ((uintptr_t)d_workspace & 255)) return entry_fail(NMT_EINVAL, "workspace must be 256-byte aligned");

@@ -465,7 +465,7 @@ __global__ __launch_bounds__(w4_waves(RM) * 64) __attribute__((amdgpu_waves_per_
     auto store = [&](auto* y) {
       using YT = std::remove_pointer_t<decltype(y)>;
       y += (row0 + 4 * q) * a.ld_y + (int64_t)tile * kW4Cols + r16;
-      const int left = rows - 4 * q, cols = a.N - tile * kW4Cols - r16;
+      const int left = rows - 4 * q, cols = tile < a.tiles ? a.N - tile * kW4Cols - r16 : 0;
 #pragma unroll
       for (int i = 0; i < RT; ++i, y += 12 * a.ld_y)
 #pragma unroll
@@ -700,10 +700,16 @@ nmt_status nmt_w4_product(const nmt_w4* w, int32_t M, const void* d_x, int32_t x
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess) return entry_fail(NMT_EDEVICE, "hipGetDevice failed");
   if (dev != w->device) return entry_fail(NMT_EINVAL, "the 4-bit matrix lives on another device than the current one");
-  const W4Args a{w->codes, w->scales, w->zeros, w->bias, w->dims.K, w->dims.N, w->kblocks, w->tiles, M, y16,
-                 d_x,      ld_x,      d_y,      ld_y};
-  const hipError_t e = launch_product(a, x16, w->dims.stype == NMT_BF16, w->gpb, w->cus, (hipStream_t)stream);
-  if (e != hipSuccess) return entry_hip_fail(e, "nmt_w4_product");
+  constexpr int kMostRows = 1 << 20;  // of a launch, whose threads are counted in 32 bits
+  for (int m0 = 0; m0 < M;) {
+    const int n = std::min(M - m0, kMostRows);
+    const W4Args a{w->codes, w->scales, w->zeros, w->bias, w->dims.K, w->dims.N, w->kblocks, w->tiles, n, y16,
+                   (const char*)d_x + (int64_t)m0 * ld_x * (x16 ? 2 : 4), ld_x,
+                   (char*)d_y + (int64_t)m0 * ld_y * (y16 ? 2 : 4), ld_y};
+    const hipError_t e = launch_product(a, x16, w->dims.stype == NMT_BF16, w->gpb, w->cus, (hipStream_t)stream);
+    if (e != hipSuccess) return entry_hip_fail(e, "nmt_w4_product");
+    m0 += n;
+  }
   return entry_ok();
 }
 

@@ -481,3 +481,16 @@ def test_two_calls_at_once():
         np.testing.assert_array_equal(acc.cpu().numpy(), want[0])
         np.testing.assert_array_equal(nxt.cpu().numpy(), want[1])
     model.close()
+
+
+@pytest.mark.parametrize("V,S,n", [(100, 1 << 22, 0), (9000, (1 << 23) + 1, 0), (9000, 1, 1 << 23), (9000, 1, 2 ** 31 - 1)])
+def test_more_rows_than_a_launch_takes(V, S, n):
+    """Refused before anything is read."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    lib = nb.load_library()
+    model = _model(nb, V)
+    a = torch.zeros(64, device="cuda").data_ptr()
+    assert lib.nmt_verify_drafts(model.handle, S, n, a, a, a, 0, V, a, 0, V, a, a, a, None, None, a, 2 ** 62, None) == nb.NMT_EINVAL
+    assert "too many" in nb.last_error()
+    model.close()

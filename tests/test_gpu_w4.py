@@ -347,3 +347,20 @@ def test_two_products_at_once():
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     w.close()
+
+
+def test_more_rows_than_a_launch_takes():
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    K, N, M = 32, 5, (1 << 21) + 3
+    c = dc.make_w4(np.random.default_rng(6), K, N, 32, True, True)
+    w = _handle(nb, c, K, N, 32)
+    x = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda")
+    at = [0, 1, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, (1 << 21) - 1, 1 << 21, M - 1]
+    few = torch.randn((len(at), K), device="cuda").bfloat16()
+    x[at] = few
+    y, want = torch.full((M, N), float("nan"), device="cuda"), torch.zeros((len(at), N), device="cuda")
+    nb.nmt_w4_product(w, x, y)
+    nb.nmt_w4_product(w, few, want)
+    assert torch.equal(y[at], want) and bool(torch.isfinite(y).all())
+    w.close()
