@@ -533,9 +533,9 @@ size_t nmt_verify_workspace_bytes(const nmt_model* m, int32_t S, int32_t n_draft
  * offsets, or that reaches a draft out of range or a row that is no
  * distribution (NaN, +infinity or nothing above -infinity), keeps the drafts
  * before it, gets d_next = -1 and log p = NaN, and sets the model's device
- * error flag.  Sequences are independent.  S = 0 is a no-op.  More than 4
- * million sequences (V <= 8192), or 16 million parts of 8,192 words of all
- * rows (larger V), are refused with NMT_EINVAL.  The call
+ * error flag.  Sequences are independent.  S = 0 is a no-op.  2^22 sequences
+ * or more, and rows of 2^24 parts of 8,192 words or more in all, are refused
+ * with NMT_EINVAL.  The call
  * allocates nothing; calls on different streams must use different workspaces.
  * d_workspace: nmt_verify_workspace_bytes bytes, 256-byte aligned.
  * Errors: NMT_EINVAL, NMT_EWORKSPACE, NMT_EDEVICE. */

@@ -12,16 +12,21 @@
 // comparison is in 64 bits: each row's sum of exponentials, the residual's
 // running sum.
 //
-// Large vocabularies take two launches.  k_row_sums reads every row once: a
-// wave takes up to 2,048 logits into registers, all loads in flight at once, a
-// block leaves a (max, sum) pair for its up to 8,192.  k_finish judges its
-// sequence from those pairs (each block by itself: 16 lanes merge a row, then a
-// lane decides a position), sums what is left of the target over its share of
-// the words, 512 at a time, and the sequence's last block to finish finds the
-// 512, then the word, whose running sum passes the random number.  Both stages
-// are spread over the whole chip, so one sequence takes no longer than its
-// share of the bandwidth; every sum has a fixed order.  Small vocabularies take
-// one launch, a block a sequence (k_verify_small).
+// As a rule there are two launches.  k_row_sums reads every row once: a wave
+// takes up to 2,048 logits into registers, all loads in flight at once, and a
+// block leaves the (max, sum) pair of up to 8,192.  It is bound by its 64-bit
+// instructions: 54 M bf16 logits (1,088 rows of 50,000) in 24.4 us, 2.2 T
+// logits/s, 128 M fp32 ones a pass in 52 us.  k_finish judges its sequence
+// from those pairs (each block by itself: 16 lanes merge a row, then a lane
+// decides a position), sums what is left of the target over its share of the
+// words, 512 at a time, and the sequence's last block to finish finds the 512,
+// then the word, whose running sum passes the random number.  It is a chain of
+// some eight dependent trips to memory (9 to 10 us for 12 sequences, three
+// quarters of its waves' time) until the rows themselves count (256 sequences
+// of 100,000 words: 205 MB in 34 us).  Both stages are spread over the whole
+// chip, so one sequence takes no longer than its share of the bandwidth; every
+// sum has a fixed order.  Few sequences over a small vocabulary take one
+// launch, a block a sequence (k_verify_small).
 #include <algorithm>
 
 #include "draft.hpp"
@@ -33,9 +38,10 @@ namespace {
 constexpr int kWavePart = 2048;   // logits of a row that one wave sums, at most
 constexpr int kWaves = 4;         // waves a block of the streaming kernels
 constexpr int kUnit = 512;        // words whose residual one wave sums at a time
-constexpr int kJudge = 8;         // positions a block judges at a time
+constexpr int kFinish = 8;        // waves a block that judges long rows ...
+constexpr int kJudge = 16;        // ... and positions it judges at a time, 16 lanes a row
+constexpr int kSmall = 8;         // positions that a block of the one-launch form judges at a time
 constexpr int kCUs = 256;
-constexpr int kSmallV = 1024 * 8; // words of the one-launch form: eight a thread
 
 // A row's (or a part's) largest logit and the sum of e^(z - max).  A NaN makes
 // the max NaN, and a row of nothing but -infinity has max -infinity and sum 0.
@@ -79,13 +85,12 @@ __device__ __forceinline__ float logit(const void* z, int is16, int64_t i) {
   return is16 ? (float)((const __bf16*)z)[i] : ((const float*)z)[i];
 }
 
-// e^x as 2^n e^r, |r| <= ln 2 / 2, e^r by the polynomial that
-// interpolates it at the Chebyshev nodes (off by at most 5.6e-11 of it, and
-// exact at 0).  14 64-bit instructions a logit, each at the rate of a 64-bit
-// multiply-add: 2 T logits/s, which keeps up with 8 TB/s of fp32 ones.  The
-// odds that a sum's error moves a decision are its part of the distance
-// between two borders: at most 5.6e-11 for a draft, and 5.6e-6 for a word out
-// of 100,000 equal ones even if every error had the same sign.
+// e^x as 2^n e^r, |r| <= ln 2 / 2, e^r by the polynomial that interpolates it
+// at the Chebyshev nodes (off by at most 5.6e-11 of it, and exact at 0), in 11
+// 64-bit instructions.  The odds that an error of the sums (at most 1e-10 of
+// them, from add_exp below) moves a decision are its part of the distance
+// between two borders: 1e-10 for a draft, and 1e-5 for a word out of 100,000
+// equal ones even if every error had the same sign.
 __device__ __forceinline__ double exp64(double x) {
   constexpr double kShift = 6755399441055744.0;  // 1.5 * 2^52: n comes out in the sum's low bits
   const double t = fma(x, 1.4426950408889634, kShift);
@@ -165,10 +170,9 @@ __device__ __forceinline__ float wave_maximum(float v) {
 // pass V the row's last eight; any alignment of the elements' own.  Returns
 // where they start: mask8 puts -infinity for those before w0.  With kShort
 // rows of less than eight words are met, of which a lane has one: each_lane()
-// words a lane.  (The type is a branch
-// here, the same for the whole wave, and not a form of each kernel: their code
-// would double, and a block that runs once waits for its instructions as for
-// its data.)
+// words a lane.  (The type is a branch here, the same for the whole wave, and
+// not a form of each kernel: their code would double, and a block that runs
+// once waits for its instructions as for its data.)
 typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
 __device__ __forceinline__ int each_lane(int V) { return V < 8 ? 1 : 8; }
 template <bool kShort>
@@ -207,11 +211,11 @@ __device__ __forceinline__ void fill_table(double* table) {
   const uint64_t j = threadIdx.x;
   if (j < 32) table[j] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, exp2((double)j / 32)) - (j << 47));
 }
-// sum + e^x for x from -700 to 700: as exp64, but in steps of ln 2 / 32 and
-// with a polynomial of degree 3 (off by at most 9.9e-11 of e^x) that a factor
-// from the table makes good: 8 64-bit instructions with the addition, and 4
-// of 32 bits.  The table's 32 doubles lie in 64 banks, one bank's worth each, so
-// lanes never wait for each other.
+// sum + e^x for x from -700 to 700: as exp64, but in steps of ln 2 / 32, so
+// that a polynomial of degree 3 does (off by at most 9.9e-11 of e^x), times a
+// factor from the table: 8 64-bit instructions with the addition, and 4 of 32
+// bits (row sums of 64 sequences: 28.5 us with exp64).  The table's 32 doubles
+// fill the 64 banks once, so lanes never wait for each other.
 constexpr float kLowest = -700.f;
 __device__ __forceinline__ double add_exp(double sum, float x, const double* table) {
   constexpr double kShift = 6755399441055744.0;
@@ -308,15 +312,15 @@ __global__ __launch_bounds__(kWaves * 64) void k_row_sums(VerifyArgs a) {
 
 // --------------------------------------------------------------- verdict
 
-// The verdict on sequence s by one block, kJudge positions at a time: fill(j0,
+// The verdict on sequence s by one block, J positions at a time: fill(j0,
 // rows) leaves the sums of their target rows and proposal rows, then the first
 // wave takes a lane a position.  With write_logp log p of each draft goes out
 // too, and every position is looked at for it.  *out holds the verdict after
 // the call, for the whole block.
-template <class Fill>
+template <int J, class Fill>
 __device__ __forceinline__ void judge(const VerifyArgs& a, int s, int o0, int o1, bool write_logp, Verdict* out,
                                       Fill&& fill) {
-  __shared__ RowSum rows[2][kJudge];
+  __shared__ RowSum rows[2][J];
   __shared__ int done;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   if (o0 < 0 || o1 < o0 || o1 > a.n_draft) {
@@ -329,10 +333,10 @@ __device__ __forceinline__ void judge(const VerifyArgs& a, int s, int o0, int o1
   }
   const int n = o1 - o0;
   if (threadIdx.x == 0) done = 0;
-  for (int j0 = 0; j0 <= n; j0 += kJudge) {
+  for (int j0 = 0; j0 <= n; j0 += J) {
     // what else a position is judged by, on its way while the sums are made
     const int j = j0 + lane;
-    const bool pos = wave == 0 && lane < kJudge && j <= n, has_p = pos && j < n && a.proposal;
+    const bool pos = wave == 0 && lane < J && j <= n, has_p = pos && j < n && a.proposal;
     const int64_t tr = (int64_t)o0 + s + j, pr = (int64_t)o0 + j;
     const int32_t d = pos && j < n ? a.draft[pr] : 0;
     const float u = pos ? a.u[tr] : 0.f;
@@ -342,7 +346,7 @@ __device__ __forceinline__ void judge(const VerifyArgs& a, int s, int o0, int o1
     fill(j0, n, rows);
     __syncthreads();
     if (wave == 0) {
-      const RowSum rt = rows[0][lane % kJudge], rp = has_p ? rows[1][lane % kJudge] : RowSum{1.0, 0.f};
+      const RowSum rt = rows[0][lane % J], rp = has_p ? rows[1][lane % J] : RowSum{1.0, 0.f};
       const bool t_ok = is_distribution(rt);
       const int bad = !d_ok ? 1 : !t_ok || !is_distribution(rp) ? 2 : 0;
       const double it = 1.0 / rt.s, ip = 1.0 / rp.s;
@@ -439,13 +443,13 @@ __device__ __forceinline__ void write_next(const VerifyArgs& a, int s, const Ver
 
 // `blocks` blocks a sequence: the verdict, the residual over every blocks-th
 // 2,048 words, and by the last to finish the word.
-__global__ __launch_bounds__(kWaves * 64) void k_finish(VerifyArgs a, int blocks) {
+__global__ __launch_bounds__(kFinish * 64) void k_finish(VerifyArgs a, int blocks) {
   __shared__ Verdict shared_v;
   __shared__ int last_block;
   const int s = blockIdx.x / blocks, b = blockIdx.x % blocks, lane = threadIdx.x & 63, wave = wave_index();
   const int o0 = a.off[s], o1 = a.off[s + 1];
   const float u = o1 >= 0 && o1 <= a.n_draft ? a.u[(int64_t)o1 + s] : 0.f;
-  judge(a, s, o0, o1, b == 0 && a.draft_logp, &shared_v, [&](int j0, int n, RowSum(&rows)[2][kJudge]) {
+  judge<kJudge>(a, s, o0, o1, b == 0 && a.draft_logp, &shared_v, [&](int j0, int n, RowSum(&rows)[2][kJudge]) {
     const int g = threadIdx.x >> 4, l16 = threadIdx.x & 15, j = j0 + g % kJudge;
     const bool prop = g >= kJudge;
     RowSum mine{0.0, -INFINITY};
@@ -498,7 +502,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_finish(VerifyArgs a, int blocks
     }
     return sum;
   };
-  int first = b * kWaves + wave, step = blocks * kWaves;
+  int first = b * kFinish + wave, step = blocks * kFinish;
   double total;
   for (;;) {
     sum_units(first, step);
@@ -514,7 +518,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_finish(VerifyArgs a, int blocks
     if (total > 0.0 || v.whole) break;
     v.whole = 1;  // nothing left: p itself, by this block
     first = wave;
-    step = kWaves;
+    step = kFinish;
   }
   if (wave != 0) return;
   // the first unit whose running sum passes the goal; where rounding has left
@@ -563,9 +567,9 @@ __global__ __launch_bounds__(kWaves * 64) void k_finish(VerifyArgs a, int blocks
 
 // ------------------------------------------------------- small vocabularies
 
-// A sequence by one block: V <= kSmallV.
-__global__ __launch_bounds__(2 * kJudge * 64) void k_verify_small(VerifyArgs a) {
-  constexpr int W = 2 * kJudge;
+// A sequence by one block: V <= kWavePart.
+__global__ __launch_bounds__(2 * kSmall * 64) void k_verify_small(VerifyArgs a) {
+  constexpr int W = 2 * kSmall;
   __shared__ Verdict shared_v;
   __shared__ double sums[2][W];
   __shared__ Picked picks[W];
@@ -574,20 +578,15 @@ __global__ __launch_bounds__(2 * kJudge * 64) void k_verify_small(VerifyArgs a) 
   __syncthreads();
   const int s = blockIdx.x, o0 = a.off[s], o1 = a.off[s + 1], lane = threadIdx.x & 63, wave = wave_index();
   const float u = o1 >= 0 && o1 <= a.n_draft ? a.u[(int64_t)o1 + s] : 0.f;
-  judge(a, s, o0, o1, a.draft_logp != nullptr, &shared_v, [&](int j0, int n, RowSum(&rows)[2][kJudge]) {
-    const bool prop = wave >= kJudge;
-    const int j = j0 + wave % kJudge;
+  judge<kSmall>(a, s, o0, o1, a.draft_logp != nullptr, &shared_v, [&](int j0, int n, RowSum(&rows)[2][kSmall]) {
+    const bool prop = wave >= kSmall;
+    const int j = j0 + wave % kSmall;
     if (j >= n + (prop ? 0 : 1) || (prop && !a.proposal)) return;
     const void* z = prop ? a.proposal : a.target;
     const int is16 = prop ? a.proposal16 : a.target16;
     const int64_t at = prop ? ((int64_t)o0 + j) * a.ld_p : ((int64_t)o0 + s + j) * a.ld_t;
-    RowSum r{0.0, -INFINITY};
-#pragma unroll 1
-    for (int i = 0; i < a.V; i += kWavePart) {
-      const RowSum p = part_sum<true>(z, is16, at, i, i + kWavePart, a.V, table);
-      r = i ? merge(r, p) : p;
-    }
-    if (lane == 0) rows[prop][wave % kJudge] = r;
+    const RowSum r = part_sum<true>(z, is16, at, 0, kWavePart, a.V, table);
+    if (lane == 0) rows[prop][wave % kSmall] = r;
   });
   Verdict v = shared_v;
   if (v.bad) {
@@ -673,18 +672,24 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   if (((uintptr_t)d_target & (target_type == NMT_BF16 ? 1 : 3)) ||
       ((uintptr_t)d_proposal & (proposal_type == NMT_BF16 ? 1 : 3)))
     return entry_fail(NMT_EINVAL, "logits must be aligned to their elements");
+  // One launch where a wave sums a row by itself and each sequence has a CU
+  // (V = 1,000: 8.4 us against 11.1 in two launches for one sequence, 16.4
+  // against 15.4 for 512; V = 4,000 and one sequence: 13.8 against 11.5), and
+  // for rows too short for the other form's loads.
+  const bool small = V < 8 || (V <= kWavePart && S <= kCUs);
   // Parts as long as the grid still gives each CU four blocks (parts four times
   // as long measured the same), and blocks of a sequence's residual until every
-  // wave has one unit or each CU four blocks, each of which judges its sequence
-  // by itself (64 sequences of 50,000 words: 45 us a call with eight, 41 with four).
+  // wave has one unit or each CU two blocks: each judges its sequence by itself
+  // (64 sequences of 50,000 words: 41.4 us a call with three, 37.4 with two, and
+  // 39.5 with twice as many blocks of four waves).
   const int64_t n_rows = (int64_t)n_draft + S + (d_proposal ? n_draft : 0);
   int part_len = kWaves * kWavePart;
   while (part_len > kLeastPart && n_rows * ceil_div(V, part_len) < 4 * kCUs) part_len /= 2;
   const int parts = ceil_div(V, part_len), units = ceil_div(V, kUnit);
   const int64_t n_parts = n_rows * parts;
-  const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, kWaves), 4 * kCUs / S));
+  const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, kFinish), 2 * kCUs / S));
   // a launch's threads are counted in 32 bits
-  if (V <= kSmallV ? S >= (1 << 22) : std::max(n_parts, (int64_t)S * blocks) >= (1 << 24))
+  if (S >= (1 << 22) || n_parts >= (1 << 24))
     return entry_fail(NMT_EINVAL, "too many rows of logits for one call");
   const VerifyWs L = verify_ws(V, S, n_draft);
   if (!d_workspace || ((uintptr_t)d_workspace & 255)) return entry_fail(NMT_EINVAL, "workspace must be 256-byte aligned");
@@ -703,11 +708,11 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, st, a, args...);
     e = hipGetLastError();
   };
-  if (V <= kSmallV) {
-    run(k_verify_small, S, 2 * kJudge * 64);
+  if (small) {
+    run(k_verify_small, S, 2 * kSmall * 64);
   } else {
     run(k_row_sums, n_parts, kWaves * 64);
-    run(k_finish, (int64_t)S * blocks, kWaves * 64, blocks);
+    run(k_finish, (int64_t)S * blocks, kFinish * 64, blocks);
   }
   if (e != hipSuccess) return entry_hip_fail(e, "nmt_verify_drafts");
   return entry_ok();

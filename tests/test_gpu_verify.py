@@ -483,14 +483,15 @@ def test_two_calls_at_once():
     model.close()
 
 
-@pytest.mark.parametrize("V,S,n", [(100, 1 << 22, 0), (9000, (1 << 23) + 1, 0), (9000, 1, 1 << 23), (9000, 1, 2 ** 31 - 1)])
+@pytest.mark.parametrize("V,S,n", [(4, 1 << 22, 0), (100, 1 << 22, 0), (9000, 1 << 22, 0), (100, 1, 1 << 23), (9000, 1, 1 << 23),
+                                   (9000, 1, 2 ** 31 - 1), (300001, 1, 300000)])
 def test_more_rows_than_a_launch_takes(V, S, n):
-    """Refused before anything is read."""
+    """Refused before anything is read (a workspace of no bytes would be, too, with another status)."""
     torch = _torch()
     from paper_1605_04809_amd import binding as nb
     lib = nb.load_library()
     model = _model(nb, V)
     a = torch.zeros(64, device="cuda").data_ptr()
-    assert lib.nmt_verify_drafts(model.handle, S, n, a, a, a, 0, V, a, 0, V, a, a, a, None, None, a, 2 ** 62, None) == nb.NMT_EINVAL
+    assert lib.nmt_verify_drafts(model.handle, S, n, a, a, a, 0, V, a, 0, V, a, a, a, None, None, a, 0, None) == nb.NMT_EINVAL
     assert "too many" in nb.last_error()
     model.close()
