@@ -201,13 +201,13 @@ struct W4Args {
 struct W4Shape {
   int rows, row_blocks, strips, wk, chunk;
 };
-// Waves a block, and K blocks in flight.  Many rows fill a CU's LDS by
-// themselves, so their block is 16 waves (80 rows of K = 500, N = 100,000: 51
-// us with 8, 32 with 16); few leave room for two blocks, and a wave for the
-// whole K of an output layer (33 rows of 1001 x 7777: 10.1 us with two K blocks
-// in flight, 9.1 with four).
-constexpr int w4_waves(int RM) { return RM > 16 ? 16 : 8; }
-constexpr int w4_depth(int RM, int GPB) { return RM > 16 || (RM == 16 && GPB == 4) ? 2 : 4; }
+// Waves a block, and K blocks in flight.  Many rows, or a K that is long for 16
+// rows, fill a CU's LDS by themselves, so their block is 16 waves (80 rows of K
+// = 500, N = 100,000: 51 us with 8, 32 with 16); the others leave room for two
+// blocks, and a wave for the whole K of an output layer (33 rows of 1001 x
+// 7777: 10.1 us with two K blocks in flight, 9.1 with four).
+constexpr int w4_waves(int RM, bool long_k) { return RM > 16 || (RM == 16 && long_k) ? 16 : 8; }
+constexpr int w4_depth(int RM, int W, int GPB) { return W > 8 || (RM == 16 && GPB == 4) ? 2 : 4; }
 
 // Eight codes of a word as fp16, minus the zero point: zl = -(1024 + z) and
 // zh = -(64 + z), twice each.  (The masks sit in registers, or the compiler
@@ -264,12 +264,12 @@ __device__ __forceinline__ float max16(float v) {
   return v;
 }
 
-template <int RM, int GPB, bool X16, bool S16>
-__global__ __launch_bounds__(w4_waves(RM) * 64) __attribute__((amdgpu_waves_per_eu(4))) void k_w4_product(
+template <int RM, int W, int GPB, bool X16, bool S16>
+__global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(4))) void k_w4_product(
     W4Args a, W4Shape sh) {
   constexpr int RT = (RM + 15) / 16;  // row tiles
   constexpr int HV = X16 ? 1 : 2;  // fp16 parts of an input
-  constexpr int D = w4_depth(RM, GPB), W = w4_waves(RM);
+  constexpr int D = w4_depth(RM, W, GPB);
   using XT = std::conditional_t<X16, __bf16, float>;
   using ST = std::conditional_t<S16, __bf16, float>;
   // [K block][step][part][lane quarter][row ^ (4 step + quarter)] fragments
@@ -482,13 +482,12 @@ __global__ __launch_bounds__(w4_waves(RM) * 64) __attribute__((amdgpu_waves_per_
 // Bytes of LDS that a K block takes.
 constexpr int w4_block_bytes(int RM, bool x16) { return RM * (x16 ? 256 : 512) + (RM + 15) / 16 * 64; }
 
-template <int RM, int GPB, bool X16, bool S16>
+template <int RM, int W, int GPB, bool X16, bool S16>
 hipError_t launch_form(const W4Args& a, const W4Shape& sh, hipStream_t st) {
   const int64_t grid = (int64_t)sh.strips * sh.row_blocks;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  const size_t lds = (size_t)sh.chunk * w4_block_bytes(RM, X16) +
-                     (sh.wk > 1 ? (size_t)w4_waves(RM) * ((RM + 15) / 16) * 64 * 16 : 0);
-  hipLaunchKernelGGL((k_w4_product<RM, GPB, X16, S16>), dim3((unsigned)grid), dim3(w4_waves(RM) * 64), lds, st, a, sh);
+  const size_t lds = (size_t)sh.chunk * w4_block_bytes(RM, X16) + (sh.wk > 1 ? (size_t)W * ((RM + 15) / 16) * 64 * 16 : 0);
+  hipLaunchKernelGGL((k_w4_product<RM, W, GPB, X16, S16>), dim3((unsigned)grid), dim3(W * 64), lds, st, a, sh);
   return hipGetLastError();
 }
 
@@ -505,12 +504,19 @@ hipError_t launch_product(const W4Args& a, bool x16, bool s16, int gpb, int cus,
   sh.row_blocks = ceil_div(tiles16, RT);
   RT = ceil_div(tiles16, sh.row_blocks);
   sh.rows = std::min(a.M, RT * 16);
-  const int RM = a.M <= 4 ? 4 : RT * 16, W = w4_waves(RM), depth = w4_depth(RM, gpb), per_cu = W > 8 ? 1 : 2;
-  const int most = std::max(1, ((per_cu == 1 ? 128 : 56) << 10) / w4_block_bytes(RM, x16));
-  // K split between waves while there are fewer than about 8 waves a CU
+  const int RM = a.M <= 4 ? 4 : RT * 16;
+  // A K that half a CU's LDS does not hold gets all of it (less the K shares'
+  // sums, which more than 16 rows never have): 5 rows of 4,000 x 1,000 in 24.0
+  // us with half and 8 waves, 9.5 with all and 16, 16 rows 25.7 and 13.3.
+  const int64_t bytes = w4_block_bytes(RM, x16);
+  const bool long_k = a.kblocks * bytes > (56 << 10);
+  const int W = w4_waves(RM, long_k), depth = w4_depth(RM, W, gpb), per_cu = W > 8 || long_k ? 1 : 2;
+  const int most = std::max<int>(1, ((per_cu == 2 ? 56 : RM > 16 ? 160 : 144) << 10) / bytes);
+  // K split between waves while there are fewer than about 8 waves a CU (a
+  // block of several row tiles has them by itself)
   const int64_t groups = groups_of(RT);
   sh.wk = 1;
-  while (sh.wk < 8 && groups * sh.wk < 8 * cus &&
+  while (sh.wk < W && groups * sh.wk < 8 * cus &&
          (most >= a.kblocks ? sh.wk * 2 <= a.kblocks : sh.wk * 2 * depth <= most))
     sh.wk *= 2;
   const int step = depth * sh.wk;
@@ -518,21 +524,24 @@ hipError_t launch_product(const W4Args& a, bool x16, bool s16, int gpb, int cus,
   // as many blocks as run at once
   const int want = ceil_div(a.tiles, W / sh.wk), fit = per_cu * cus / sh.row_blocks;
   sh.strips = want <= fit ? (int)round_up(want, 8) : std::max(fit / 8 * 8, 8);
-  auto types = [&](auto rm, auto g) {
-    constexpr int R = decltype(rm)::value, G = decltype(g)::value;
-    return x16 ? (s16 ? launch_form<R, G, true, true>(a, sh, st) : launch_form<R, G, true, false>(a, sh, st))
-               : (s16 ? launch_form<R, G, false, true>(a, sh, st) : launch_form<R, G, false, false>(a, sh, st));
+  auto types = [&](auto rm, auto w, auto g) {
+    constexpr int R = decltype(rm)::value, V = decltype(w)::value, G = decltype(g)::value;
+    return x16 ? (s16 ? launch_form<R, V, G, true, true>(a, sh, st) : launch_form<R, V, G, true, false>(a, sh, st))
+               : (s16 ? launch_form<R, V, G, false, true>(a, sh, st) : launch_form<R, V, G, false, false>(a, sh, st));
   };
-  auto form = [&](auto rm) {
-    return gpb == 4   ? types(rm, std::integral_constant<int, 4>{})
-           : gpb == 2 ? types(rm, std::integral_constant<int, 2>{})
-                      : types(rm, std::integral_constant<int, 1>{});
+  auto form = [&](auto rm, auto w) {
+    return gpb == 4   ? types(rm, w, std::integral_constant<int, 4>{})
+           : gpb == 2 ? types(rm, w, std::integral_constant<int, 2>{})
+                      : types(rm, w, std::integral_constant<int, 1>{});
   };
+  using std::integral_constant;
   switch (RM) {
-    case 4: return form(std::integral_constant<int, 4>{});
-    case 16: return form(std::integral_constant<int, 16>{});
-    case 32: return form(std::integral_constant<int, 32>{});
-    default: return form(std::integral_constant<int, 48>{});
+    case 4: return form(integral_constant<int, 4>{}, integral_constant<int, 8>{});
+    case 16:
+      return W == 8 ? form(integral_constant<int, 16>{}, integral_constant<int, 8>{})
+                    : form(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+    case 32: return form(integral_constant<int, 32>{}, integral_constant<int, 16>{});
+    default: return form(integral_constant<int, 48>{}, integral_constant<int, 16>{});
   }
 }
 
