@@ -251,17 +251,21 @@ __device__ __forceinline__ void load8(const __bf16* x, int n, float (&v)[8]) {
   }
 }
 
-// The largest of 16 consecutive lanes' values, in all of them.
-__device__ __forceinline__ float max16(float v) {
+// The largest magnitude of 16 consecutive lanes' eight values, as a float's
+// bits (a NaN's lie above infinity's).
+__device__ __forceinline__ uint32_t largest16(const float (&v)[8]) {
+  float f = __builtin_elementwise_maximum(fabsf(v[0]), fabsf(v[1]));  // (NaN if either is)
+#pragma unroll
+  for (int e = 2; e < 8; ++e) f = __builtin_elementwise_maximum(f, fabsf(v[e]));
+  uint32_t m = __builtin_bit_cast(uint32_t, f) & 0x7fffffffu;
   auto with = [&](auto ctrl) {
-    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf,
-                                                                    0xf, true)));
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, decltype(ctrl)::value, 0xf, 0xf, true));
   };
   with(std::integral_constant<int, 0xB1>{});   // lane ^ 1
   with(std::integral_constant<int, 0x4E>{});   // lane ^ 2
   with(std::integral_constant<int, 0x141>{});  // 7 - lane of 8
   with(std::integral_constant<int, 0x140>{});  // 15 - lane of 16
-  return v;
+  return m;
 }
 
 template <int RM, int W, int GPB, bool X16, bool S16>
@@ -313,37 +317,23 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(4))) voi
 
   // Eight inputs of a K block that 16 lanes hold to LDS; returns the block's 2^-e
   auto convert = [&](const float (&v)[8], f32x4* to) {
-    float mx = 0.f;  // (fmaxf passes over NaN, which is NaN at any scale)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(v[e]));
-    mx = max16(mx);
-    const bool infinite = __ballot(mx == INFINITY) != 0;
+    constexpr uint32_t kInf = 0x7f800000u;
+    uint32_t mx = largest16(v);  // (a NaN makes all of its row's outputs NaN, at any scale)
+    const bool infinite = __ballot(mx == kInf) != 0;
     if (infinite) {  // the largest of the finite ones
-      mx = 0.f;
+      float w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mx = fabsf(v[e]) < INFINITY ? fmaxf(mx, fabsf(v[e])) : mx;
-      mx = max16(mx);
+      for (int e = 0; e < 8; ++e) w[e] = fabsf(v[e]) < INFINITY ? v[e] : 0.f;
+      mx = largest16(w);
     }
     // 2^e puts the largest in [2^14, 2^15); e not above 120, so that 2^-e is normal
-    const int e2 = mx > 0.f ? min(15 - __builtin_amdgcn_frexp_expf(mx), 120) : 0;
+    const int e2 = mx - 1 < kInf - 1 ? min(15 - __builtin_amdgcn_frexp_expf(__builtin_bit_cast(float, mx)), 120) : 0;
     const float up = __builtin_amdgcn_ldexpf(1.f, e2);
     f16x8 hi, lo;
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      f32x2 f;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f[u] = v[e + u] * up;
-        // (kept in a register, or it is rounded to fp16 a second time for the remainder)
-        if constexpr (HV == 2) asm("" : "+v"(f[u]));
-      }
-      const f16x2 h = __builtin_convertvector(f, f16x2);
-      hi[e] = h[0];
-      hi[e + 1] = h[1];
-      if constexpr (HV == 2) {
-        lo[e] = (_Float16)(f[0] - (float)h[0]);
-        lo[e + 1] = (_Float16)(f[1] - (float)h[1]);
-      }
+    for (int e = 0; e < 8; ++e) {
+      hi[e] = (_Float16)(v[e] * up);
+      if constexpr (HV == 2) lo[e] = (_Float16)fmaf(v[e], up, -(float)hi[e]);
     }
     if constexpr (HV == 2)
       if (infinite)  // an infinity is all in hi (inf - inf is no remainder)
@@ -359,20 +349,29 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(4))) voi
   const XT* x = (const XT*)a.x + (int64_t)row0 * a.ld_x;
   float* units = (float*)(lds + sh.chunk * 16 * HV * RM);
   auto stage = [&](int kb0, int nkb) {
-    for (int p0 = tid >> 4; p0 < rows * nkb; p0 += U * kTakers) {
+    const int dm = kTakers / nkb, dk = kTakers % nkb;
+    for (int m = (tid >> 4) / nkb, kl = (tid >> 4) % nkb; m < rows;) {
       float v[U][8];
+      int mu[U], ku[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int p = p0 + u * kTakers, m = p / nkb, k = (kb0 + p % nkb) * kW4Rows + r16 * 8;
-        load8(x + m * a.ld_x + k, p < rows * nkb ? a.K - k : 0, v[u]);
+        const int k = (kb0 + kl) * kW4Rows + r16 * 8;
+        load8(x + m * a.ld_x + k, m < rows ? a.K - k : 0, v[u]);
+        mu[u] = m;
+        ku[u] = kl;
+        m += dm;
+        kl += dk;
+        if (kl >= nkb) {
+          kl -= nkb;
+          ++m;
+        }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int p = p0 + u * kTakers, m = p / nkb, kl = p % nkb;
-        if (p >= rows * nkb) break;
-        f32x4* to = lds + ((kl * 4 + (r16 >> 2)) * HV * 4 + (r16 & 3)) * RM + (RM < 16 ? m : m ^ r16);
+        if (mu[u] >= rows) break;
+        f32x4* to = lds + ((ku[u] * 4 + (r16 >> 2)) * HV * 4 + (r16 & 3)) * RM + (RM < 16 ? mu[u] : mu[u] ^ r16);
         const float unit = convert(v[u], to);
-        if (r16 == 0) units[kl * (16 * RT) + m] = unit;
+        if (r16 == 0) units[ku[u] * (16 * RT) + mu[u]] = unit;
       }
     }
   };
