@@ -167,122 +167,147 @@ __device__ __forceinline__ float wave_maximum(float v) {
 }
 
 // Eight consecutive logits of the row at z[row], from w0, or where those would
-// pass V the row's last eight; any alignment of the elements' own.  Returns
-// where they start: mask8 puts -infinity for those before w0.  With kShort
-// rows of less than eight words are met, of which a lane has one: each_lane()
-// words a lane.  (The type is a branch here, the same for the whole wave, and
-// not a form of each kernel: their code would double, and a block that runs
-// once waits for its instructions as for its data.)
-typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
+// pass V the row's last eight; any alignment of the elements' own.  They come
+// as they are in memory (bf16 ones in x[0 .. 3]), so that nothing waits for
+// them before ready8, which makes floats of them, -infinity for those before
+// w0.  Returns where they start.  With kShort rows of less than eight words are
+// met, of which a lane has one: each_lane() words a lane.  (The type is a branch
+// here, the same for the whole wave, and not a form of each kernel: their code
+// would double, and a block that runs once waits for its instructions as for
+// its data.)
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ float as_float(uint32_t u) { return __builtin_bit_cast(float, u); }
 __device__ __forceinline__ int each_lane(int V) { return V < 8 ? 1 : 8; }
 template <bool kShort>
-__device__ __forceinline__ int load8(const void* z, int is16, int64_t row, int w0, int V, float (&x)[8]) {
+__device__ __forceinline__ int load8(const void* z, int is16, int64_t row, int w0, int V, f32x8& x) {
   if (kShort && V < 8) {
-    x[0] = w0 < V ? logit(z, is16, row + w0) : -INFINITY;
-#pragma unroll
-    for (int e = 1; e < 8; ++e) x[e] = -INFINITY;
+    x = is16 ? as_float(0xff80ff80u) : -INFINITY;
+    if (is16)
+      x[0] = as_float(0xff800000u | (w0 < V ? ((const uint16_t*)z)[row + w0] : 0xff80u));
+    else
+      x[0] = w0 < V ? ((const float*)z)[row + w0] : -INFINITY;
     return w0;
   }
   const int at = min(w0, V - 8);
   if (is16) {
-    const bf16x8u a = *(const bf16x8u*)((const __bf16*)z + row + at);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)a[e];
+    typedef float f32x4h __attribute__((ext_vector_type(4), aligned(2)));
+    const f32x4h a = *(const f32x4h*)((const uint16_t*)z + row + at);
+    x = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
   } else {
     const f32x4u* p = (const f32x4u*)((const float*)z + row + at);
     const f32x4u a = p[0], b = p[1];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = e < 4 ? a[e] : b[e - 4];
+    x = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   }
   return at;
 }
-__device__ __forceinline__ void mask8(int at, int w0, float (&x)[8]) {
-  if (at < w0) {
+__device__ __forceinline__ void ready8(int is16, int at, int w0, f32x8& x) {
+  if (is16) {
+    f32x8 y;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = at + e < w0 ? -INFINITY : x[e];
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t u = __float_as_uint(x[e / 2]);
+      y[e] = as_float(e & 1 ? u & 0xffff0000u : u << 16);
+    }
+    x = y;
+  }
+  if (at < w0) {
+    f32x8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = at + e < w0 ? -INFINITY : x[e];
+    x = y;
   }
 }
 
 // ------------------------------------------------------------- row sums
 
-// 2^(j / 32) into table[j], less j << 15 in the upper half: n << 15 on that
-// puts n / 32 on the exponent, whole steps alone.
-__device__ __forceinline__ void fill_table(double* table) {
-  const uint64_t j = threadIdx.x;
-  if (j < 32) table[j] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, exp2((double)j / 32)) - (j << 47));
-}
+// 2^(j / 32) as a double's bits, less j << 15 in the upper half: n << 15 on
+// that puts n / 32 on the exponent, whole steps alone.
+__device__ const uint64_t kPowers[32] = {
+    0x3ff0000000000000, 0x3fefd9b0d3158574, 0x3fefb5586cf9890f, 0x3fef9301d0125b51,
+    0x3fef72b83c7d517b, 0x3fef54873168b9aa, 0x3fef387a6e756238, 0x3fef1e9df51fdee1,
+    0x3fef06fe0a31b715, 0x3feef1a7373aa9cb, 0x3feedea64c123422, 0x3feece086061892d,
+    0x3feebfdad5362a27, 0x3feeb42b569d4f82, 0x3feeab07dd485429, 0x3feea47eb03a5585,
+    0x3feea09e667f3bcd, 0x3fee9f75e8ec5f74, 0x3feea11473eb0187, 0x3feea589994cce13,
+    0x3feeace5422aa0db, 0x3feeb737b0cdc5e5, 0x3feec49182a3f090, 0x3feed503b23e255d,
+    0x3feee89f995ad3ad, 0x3feeff76f2fb5e47, 0x3fef199bdd85529c, 0x3fef3720dcef9069,
+    0x3fef5818dcfba487, 0x3fef7c97337b9b5f, 0x3fefa4afa2a490da, 0x3fefd0765b6e4540,
+};
 // sum + e^x for x from -700 to 700: as exp64, but in steps of ln 2 / 32, so
 // that a polynomial of degree 3 does (off by at most 9.9e-11 of e^x), times a
 // factor from the table: 8 64-bit instructions with the addition, and 4 of 32
 // bits (row sums of 64 sequences: 28.5 us with exp64).  The table's 32 doubles
 // fill the 64 banks once, so lanes never wait for each other.
 constexpr float kLowest = -700.f;
-__device__ __forceinline__ double add_exp(double sum, float x, const double* table) {
+__device__ __forceinline__ double add_exp(double sum, float x, const uint64_t* table) {
   constexpr double kShift = 6755399441055744.0;
   const double d = maximum(x, kLowest);
   const double t = fma(d, 46.16624130844683, kShift);
   const double r = fma(t - kShift, -0.02166084939249829, d);
   const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
-  const uint64_t b = __builtin_bit_cast(uint64_t, table[n & 31]);
+  const uint64_t b = table[n & 31];
   uint32_t hi;  // (the compiler would take a 64-bit addition for it)
   asm("v_lshl_add_u32 %0, %1, 15, %2" : "=v"(hi) : "v"(n), "v"((uint32_t)(b >> 32)));
   const double p = fma(fma(fma(0.16666804903930896, r, 0.5000040488943809), r, 0.9999999999525067), r, 1.0);
   return fma(__builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)b), p, sum);
 }
 
-// The pair of up to kWavePart logits of a row, from word `from` to `to` or the
-// row's end, by one wave.  A largest of ordinary size is not taken off each
-// logit but divided out of their sum: its own term still counts exactly 1.
+// Up to kWavePart logits of a row, from word `from` to `to` or the row's end,
+// on their way to one wave, and their pair.  A largest of ordinary size is not
+// taken off each logit but divided out of their sum: its own term still counts
+// exactly 1.
 constexpr float kPlain = 200.f;  // 2,048 e^200 and e^-200 are far inside a double's range
 constexpr int kSteps = kWavePart / 512;  // eight logits a lane and step
 template <bool kShort>
-__device__ __forceinline__ RowSum part_sum(const void* z, int is16, int64_t row, int from, int to, int V,
-                                           const double* table) {
-  const int w0 = from + (int)(threadIdx.x & 63) * (kShort ? each_lane(V) : 8);
-  float x[kSteps][8], m = -INFINITY;
+struct Part {
+  const void* z;
+  int is16, from, to, V, w0;
+  int64_t row;
+  f32x8 x[kSteps];
   int at[kSteps];
-  to = min(to, V);
-  auto load = [&](int type) {
+
+  __device__ __forceinline__ Part(const void* z, int is16, int64_t row, int from, int to, int V)
+      : z(z), is16(is16), from(from), to(min(to, V)), V(V),
+        w0(from + (int)(threadIdx.x & 63) * (kShort ? each_lane(V) : 8)), row(row) {
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)
-      if (from + i * 512 < to) at[i] = load8<kShort>(z, type, row, w0 + i * 512, V, x[i]);
-  };
-  if (is16)
-    load(1);
-  else
-    load(0);
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    if (from + i * 512 >= to) break;  // (a short part has few steps)
-    mask8(at[i], w0 + i * 512, x[i]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = maximum(m, x[i][e]);
+      if (this->from + i * 512 < this->to) at[i] = load8<kShort>(z, is16, row, w0 + i * 512, V, x[i]);
   }
-  m = wave_maximum(m);
-  double s = 0.0;
-  if (m >= -kPlain && m <= kPlain) {
-    double s1 = 0.0;
+
+  __device__ __forceinline__ RowSum sum(const uint64_t* table) {
+    float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      if (from + i * 512 >= to) break;
+      if (from + i * 512 >= to) break;  // (a short part has few steps)
+      ready8(is16, at[i], w0 + i * 512, x[i]);
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        s = add_exp(s, x[i][e], table);
-        s1 = add_exp(s1, x[i][e + 1], table);
+      for (int e = 0; e < 8; ++e) m = maximum(m, x[i][e]);
+    }
+    m = wave_maximum(m);
+    double s = 0.0;
+    if (m >= -kPlain && m <= kPlain) {
+      double s1 = 0.0;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        if (from + i * 512 >= to) break;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          s = add_exp(s, x[i][e], table);
+          s1 = add_exp(s1, x[i][e + 1], table);
+        }
       }
-    }
-    s = wave_sum(s + s1) / add_exp(0.0, m, table);
-  } else if (m > -INFINITY && m < INFINITY) {
+      s = wave_sum(s + s1) / add_exp(0.0, m, table);
+    } else if (m > -INFINITY && m < INFINITY) {
 #pragma unroll 1
-    for (int i = 0; from + i < to; i += 512) {
-      mask8(load8<kShort>(z, is16, row, w0 + i, V, x[0]), w0 + i, x[0]);
+      for (int i = 0; from + i < to; i += 512) {
+        ready8(is16, load8<kShort>(z, is16, row, w0 + i, V, x[0]), w0 + i, x[0]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += exp_rel(x[0][e], m);
+        for (int e = 0; e < 8; ++e) s += exp_rel(x[0][e], m);
+      }
+      s = wave_sum(s);
     }
-    s = wave_sum(s);
+    return RowSum{s, m};
   }
-  return RowSum{s, m};
-}
+};
 
 __device__ __forceinline__ RowSum merge(const RowSum& a, const RowSum& b) {
   const float m = maximum(a.m, b.m);
@@ -293,9 +318,7 @@ __device__ __forceinline__ RowSum merge(const RowSum& a, const RowSum& b) {
 // One block per part of a row.
 __global__ __launch_bounds__(kWaves * 64) void k_row_sums(VerifyArgs a) {
   __shared__ RowSum sums[kWaves];
-  __shared__ double table[32];
-  fill_table(table);
-  __syncthreads();
+  __shared__ uint64_t table[32];
   const int64_t row = blockIdx.x / a.parts;
   const int part = blockIdx.x % a.parts, wave = wave_index();
   const int64_t thread = (int64_t)blockIdx.x * (kWaves * 64) + threadIdx.x;
@@ -303,8 +326,12 @@ __global__ __launch_bounds__(kWaves * 64) void k_row_sums(VerifyArgs a) {
   const int64_t n_target = (int64_t)a.n_draft + a.S;
   const bool tgt = row < n_target;
   const int from = part * a.part_len + wave * (a.part_len / kWaves);
-  const RowSum r = part_sum<false>(tgt ? a.target : a.proposal, tgt ? a.target16 : a.proposal16,
-                            tgt ? row * a.ld_t : (row - n_target) * a.ld_p, from, from + a.part_len / kWaves, a.V, table);
+  const uint64_t power = kPowers[threadIdx.x & 31];  // (before the logits, or it waits for them)
+  Part<false> part_of(tgt ? a.target : a.proposal, tgt ? a.target16 : a.proposal16,
+                      tgt ? row * a.ld_t : (row - n_target) * a.ld_p, from, from + a.part_len / kWaves, a.V);
+  if (threadIdx.x < 32) table[threadIdx.x] = power;
+  __syncthreads();
+  const RowSum r = part_of.sum(table);
   if ((threadIdx.x & 63) == 0) sums[wave] = r;
   __syncthreads();
   if (threadIdx.x == 0) a.rows[blockIdx.x] = merge(merge(sums[0], sums[1]), merge(sums[2], sums[3]));
@@ -379,7 +406,7 @@ __device__ __forceinline__ void write_bad(const VerifyArgs& a, int s, const Verd
 // What is left of eight words for the draw: those from w0, or the last eight,
 // in which those before w0 count nothing.  `at` is where they start.
 struct Logits8 {
-  float t[8], p[8];
+  f32x8 t, p;
   int at;
 };
 __device__ __forceinline__ bool minus_proposal(const Verdict& v) { return v.p_row >= 0 && !v.whole; }
@@ -388,13 +415,14 @@ __device__ __forceinline__ void load_residual8(const VerifyArgs& a, const Verdic
   x.at = load8<kShort>(a.target, a.target16, v.t_row * a.ld_t, w0, a.V, x.t);
   if (minus_proposal(v)) load8<kShort>(a.proposal, a.proposal16, v.p_row * a.ld_p, w0, a.V, x.p);
 }
-__device__ __forceinline__ void residual8(const Verdict& v, int w0, Logits8& x, double (&r)[8]) {
-  mask8(x.at, w0, x.t);
+__device__ __forceinline__ void residual8(const VerifyArgs& a, const Verdict& v, int w0, Logits8& x, double (&r)[8]) {
+  ready8(a.target16, x.at, w0, x.t);
 #pragma unroll
   for (int e = 0; e < 8; ++e) r[e] = exp_rel(x.t[e], v.mt) * v.it;
   if (minus_proposal(v)) {
     // (both products rounded, and not one inside a multiply-add: equal rows leave nothing)
 #pragma clang fp contract(off)
+    ready8(a.proposal16, x.at, w0, x.p);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const double q = exp_rel(x.p[e], v.mp) * v.ip;
@@ -478,7 +506,7 @@ __global__ __launch_bounds__(kFinish * 64) void k_finish(VerifyArgs a, int block
       if (i < a.units) load_residual8<false>(a, v, i * kUnit + lane * 8, next);
       if (now >= 0) {
         double r[8];
-        residual8(v, now * kUnit + lane * 8, x, r);
+        residual8(a, v, now * kUnit + lane * 8, x, r);
         const double sum = wave_sum(sum8(r));
         if (lane == 0) __hip_atomic_store(rest + now, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
@@ -559,7 +587,7 @@ __global__ __launch_bounds__(kFinish * 64) void k_finish(VerifyArgs a, int block
   double r[8];
   Logits8 x;
   load_residual8<false>(a, v, w0, x);
-  residual8(v, w0, x, r);
+  residual8(a, v, w0, x, r);
   const double scan = wave_scan(sum8(r));
   const Picked p = pick_wave(pick8(r, run + lane_before(scan), goal, x.at));
   if (lane == 0) write_next(a, s, v, p.hit != kNone ? p.hit : p.last);
@@ -573,8 +601,8 @@ __global__ __launch_bounds__(2 * kSmall * 64) void k_verify_small(VerifyArgs a) 
   __shared__ Verdict shared_v;
   __shared__ double sums[2][W];
   __shared__ Picked picks[W];
-  __shared__ double table[32];
-  fill_table(table);
+  __shared__ uint64_t table[32];
+  if (threadIdx.x < 32) table[threadIdx.x] = kPowers[threadIdx.x];
   __syncthreads();
   const int s = blockIdx.x, o0 = a.off[s], o1 = a.off[s + 1], lane = threadIdx.x & 63, wave = wave_index();
   const float u = o1 >= 0 && o1 <= a.n_draft ? a.u[(int64_t)o1 + s] : 0.f;
@@ -585,7 +613,7 @@ __global__ __launch_bounds__(2 * kSmall * 64) void k_verify_small(VerifyArgs a) 
     const void* z = prop ? a.proposal : a.target;
     const int is16 = prop ? a.proposal16 : a.target16;
     const int64_t at = prop ? ((int64_t)o0 + j) * a.ld_p : ((int64_t)o0 + s + j) * a.ld_t;
-    const RowSum r = part_sum<true>(z, is16, at, 0, kWavePart, a.V, table);
+    const RowSum r = Part<true>(z, is16, at, 0, kWavePart, a.V).sum(table);
     if (lane == 0) rows[prop][wave % kSmall] = r;
   });
   Verdict v = shared_v;
@@ -601,7 +629,7 @@ __global__ __launch_bounds__(2 * kSmall * 64) void k_verify_small(VerifyArgs a) 
     v.whole = pass;
     if (wave == 0 || wave * 512 < a.V) {
       load_residual8<true>(a, v, w0, x);
-      residual8(v, w0, x, r);
+      residual8(a, v, w0, x, r);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) r[e] = 0.0;
