@@ -14,19 +14,20 @@
 //
 // As a rule there are two launches.  k_row_sums reads every row once: a wave
 // takes up to 2,048 logits into registers, all loads in flight at once, and a
-// block leaves the (max, sum) pair of up to 8,192.  It is bound by its 64-bit
-// instructions: 54 M bf16 logits (1,088 rows of 50,000) in 24.4 us, 2.2 T
-// logits/s, 128 M fp32 ones a pass in 52 us.  k_finish judges its sequence
-// from those pairs (each block by itself: 16 lanes merge a row, then a lane
-// decides a position), sums what is left of the target over its share of the
-// words, 512 at a time, and the sequence's last block to finish finds the 512,
-// then the word, whose running sum passes the random number.  It is a chain of
-// some eight dependent trips to memory (9 to 10 us for 12 sequences, three
-// quarters of its waves' time) until the rows themselves count (256 sequences
-// of 100,000 words: 205 MB in 34 us).  Both stages are spread over the whole
-// chip, so one sequence takes no longer than its share of the bandwidth; every
-// sum has a fixed order.  Few sequences over a small vocabulary take one
-// launch, a block a sequence (k_verify_small).
+// block leaves the (max, sum) pair of up to 8,192.  fp32 rows keep it at the
+// rate of memory (79 M logits, 317 MB, in 50 us), bf16 ones at that of its
+// 64-bit instructions (30 M logits in 22.5 us, 15 of them VALU; parts half or
+// twice as long: 1 and 3 us more).  k_finish judges its sequence from those
+// pairs (each block by itself: 16 lanes merge a row, then a lane decides a
+// position), sums what is left of the target over its share of the words, 512
+// at a time, and the sequence's last block to finish finds the 512, then the
+// word, whose running sum passes the random number.  It is a chain of some
+// eight dependent trips to memory (9 to 10 us for 12 sequences, three quarters
+// of its waves' time) until the rows themselves count (256 sequences of 100,000
+// words: 102 MB in 32 us).  Both stages are spread over the whole chip, so one
+// sequence takes no longer than its share of the bandwidth; every sum has a
+// fixed order.  Few sequences over a small vocabulary take one launch, a block
+// a sequence (k_verify_small).
 #include <algorithm>
 
 #include "draft.hpp"

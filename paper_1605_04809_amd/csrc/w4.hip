@@ -178,10 +178,15 @@ __global__ __launch_bounds__(256) void k_w4_out_codes(const void* __restrict__ W
 // 1024 + 16 n).  Lane 16 q + r holds column r of a tile, so it needs one scale
 // and one zero point a group.  WK > 1 splits K between waves where there are
 // few columns; their sums meet in LDS in a fixed order.
+//
+// Measured, a call: 1 row of K = 500, N = 100,000 9.5 us (29 MB; its loads
+// alone 5.5), 12 rows of N = 50,000 in groups of 32 8.0, 4 bf16 rows of 4096 x
+// 4096 6.0, 32 inputs to 1,000 outputs 4.2 on the GPU: launch, first loads and
+// the inputs' conversion.  80 rows of N = 100,000 30 us, bound by what the
+// SIMDs issue: 114 VALU instructions beside the 16 MFMA steps of 32 rows x 16
+// columns x 128 (16.7 us; the loads alone 9.5, staging 2.5, stores 4).
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-
 
 struct W4Args {
   const uint4* codes;
