@@ -495,3 +495,17 @@ def test_more_rows_than_a_launch_takes(V, S, n):
     assert lib.nmt_verify_drafts(model.handle, S, n, a, a, a, 0, V, a, 0, V, a, a, a, None, None, a, 0, None) == nb.NMT_EINVAL
     assert "too many" in nb.last_error()
     model.close()
+
+
+@pytest.mark.parametrize("V", [1, 2, 5, 7, 8, 9, 15])
+@pytest.mark.parametrize("tt,pt", [("bfloat16", "bfloat16"), ("float32", "bfloat16"), ("bfloat16", "float32")])
+@pytest.mark.parametrize("S,pad,shift", [(6, 0, 0), (6, 3, 1), (300, 1, 1)])
+def test_rows_of_few_words(V, tt, pt, S, pad, shift):
+    """Rows shorter than the eight words that a lane reads at once, and of one or two such."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    model = _model(nb, V)
+    ins = _inputs(np.random.default_rng(V + S), V, S, 3, tt == "bfloat16", pt == "bfloat16", near=1.5)
+    _same(_run(torch, nb, model, *ins, tt=tt, pt=pt, pad=pad, shift=shift), dc.verify(*ins), ins[2])
+    assert nb.nmt_stream_status(model) == nb.NMT_OK
+    model.close()
