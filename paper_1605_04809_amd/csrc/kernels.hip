@@ -1249,14 +1249,26 @@ __global__ __launch_bounds__(VocabTune<P>::VNW * 64) void k_vocab_lse(const floa
   // Stationary activation tile: As[kq][m] = vector kq of row m0 + m, with
   // the bias slots set to 1.  Staged after the first weight loads went out,
   // so their latency and the tile's overlap.
-  for (int idx = threadIdx.x; idx < KQ * VTM; idx += VNW * 64) {
-    const int m = idx % VTM, kq = idx / VTM, row = m0 + m;
-    As[kq * VTM + m] = with_bias_ones<P>(
-        load_a_vec<P>(row >= M ? nullptr
-                      : t16    ? (const char*)((const __bf16*)t + (int64_t)row * bf16_row(E))
-                               : (const char*)(t + (int64_t)row * E),
-                      t16, E, kq * P::KV),
-        kq, E, nb);
+  if constexpr (OUT) {
+    // (few rows are shared by all threads: 5 rows of E = 500 take one trip to memory, not 16)
+    const int rows = min(VTM, M - m0);
+    for (int idx = threadIdx.x; idx < KQ * rows; idx += VNW * 64) {
+      const int m = idx % rows, kq = idx / rows;
+      As[kq * VTM + m] =
+          with_bias_ones<P>(load_a_vec<P>((const char*)(t + (int64_t)(m0 + m) * E), 0, E, kq * P::KV), kq, E, nb);
+    }
+    for (int idx = threadIdx.x; idx < KQ * VTM; idx += VNW * 64)
+      if (idx % VTM >= rows) As[idx] = zero4();
+  } else {
+    for (int idx = threadIdx.x; idx < KQ * VTM; idx += VNW * 64) {
+      const int m = idx % VTM, kq = idx / VTM, row = m0 + m;
+      As[kq * VTM + m] = with_bias_ones<P>(
+          load_a_vec<P>(row >= M ? nullptr
+                        : t16    ? (const char*)((const __bf16*)t + (int64_t)row * bf16_row(E))
+                                 : (const char*)(t + (int64_t)row * E),
+                        t16, E, kq * P::KV),
+          kq, E, nb);
+    }
   }
   __syncthreads();
   const f32x4* arow = As + h * VTM + l32;  // + 2*kg*VTM per k group
