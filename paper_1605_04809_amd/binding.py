@@ -224,20 +224,26 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_ROW_TYPES = {}   # torch dtype -> nmt_dtype (filled on first use: torch is imported late)
+
+
 def _rows(t, cols: int, rows: int):
     """(address, element type, row stride) of a device matrix of fp32 or bf16
     rows; the elements of a row must be consecutive."""
-    import torch
-    types = {torch.float32: NMT_F32, torch.bfloat16: NMT_BF16}
+    if not _ROW_TYPES:
+        import torch
+        _ROW_TYPES.update({torch.float32: NMT_F32, torch.bfloat16: NMT_BF16})
     if not t.is_cuda:
         raise ValueError("expected a device tensor")
-    if t.dtype not in types:
+    kind = _ROW_TYPES.get(t.dtype)
+    if kind is None:
         raise ValueError(f"expected fp32 or bf16 elements, got {t.dtype}")
-    if t.dim() != 2 or tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols):
         raise ValueError(f"expected a [{rows}, {cols}] tensor, got {tuple(t.shape)}")
-    if cols > 1 and t.stride(1) != 1:
+    step, one = t.stride()
+    if one != 1 and cols > 1:
         raise ValueError("expected rows of consecutive elements")
-    return t.data_ptr(), types[t.dtype], t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    return t.data_ptr(), kind, step if rows > 1 else max(cols, step)
 
 
 def _checked(t, dtype, n: int, what: str):
