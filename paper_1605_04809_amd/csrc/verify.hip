@@ -545,7 +545,8 @@ __global__ __launch_bounds__(kFinish * 64) void k_finish(VerifyArgs a, int block
     }
     total = running([](int, const double(&)[4], double) {});
     if (total > 0.0 || v.whole) break;
-    v.whole = 1;  // nothing left: p itself, by this block
+    __syncthreads();  // (every wave has read the sums that the next pass replaces, and all of them the same)
+    v.whole = 1;      // nothing left: p itself, by this block
     first = wave;
     step = kFinish;
   }

@@ -509,3 +509,33 @@ def test_rows_of_few_words(V, tt, pt, S, pad, shift):
     _same(_run(torch, nb, model, *ins, tt=tt, pt=pt, pad=pad, shift=shift), dc.verify(*ins), ins[2])
     assert nb.nmt_stream_status(model) == nb.NMT_OK
     model.close()
+
+
+@pytest.mark.parametrize("V,S", [(9000, 40), (140001, 12), (300001, 3)])
+def test_nothing_left_of_many_rows(V, S):
+    """Every sequence's residual is nothing, so that the sums of one pass are
+    replaced by another's while waves of the block may still read them: p
+    itself, call after call on one workspace."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    model = _model(nb, V)
+    rng = np.random.default_rng(V)
+    off = np.arange(S + 1).astype(np.int32)
+    draft = rng.integers(0, V, size=S).astype(np.int32)
+    target = rng.standard_normal((2 * S, V)).astype(np.float32)
+    target[2 * np.arange(S), draft] = -np.inf
+    prop = target[0::2].copy()
+    u = rng.random(2 * S, dtype=np.float32)
+    want = dc.verify(off, draft, target, prop, u)
+    assert not want[0].any()
+    d = [_dev(torch, a) for a in (off, draft, target, prop, u)]
+    acc, nxt = (torch.zeros(S, dtype=torch.int32, device="cuda") for _ in range(2))
+    ws = torch.empty(nb.nmt_verify_workspace_bytes(model, S, S), dtype=torch.uint8, device="cuda")
+    for i in range(30):
+        acc.fill_(-7)
+        nxt.fill_(-7)
+        nb.nmt_verify_drafts(model, *d, acc, nxt, workspace=ws)
+        np.testing.assert_array_equal(acc.cpu().numpy(), want[0], err_msg=f"call {i}")
+        np.testing.assert_array_equal(nxt.cpu().numpy(), want[1], err_msg=f"call {i}")
+    assert nb.nmt_stream_status(model) == nb.NMT_OK
+    model.close()
