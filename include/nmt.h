@@ -437,7 +437,8 @@ nmt_status nmt_step_readouts(nmt_model* m, const nmt_source* src, int32_t B, con
  *                     NaN gets logits that are not finite.
  *   d_logits          out: row i at d_logits + i * ld_logits, V fp32 values
  *                     (ld_logits >= V; what lies between rows is not written)
- *   d_logZ [M]        out, nullable: log sum_v exp(z_v)
+ *   d_logZ [M]        out, nullable: log sum_v exp(z_v); NaN where a logit is, else
+ *                     infinity where one is
  * Workspace as for nmt_score_batch with B = M.  Rows are independent.  M = 0
  * is a no-op.  Errors: NMT_EINVAL, NMT_EWORKSPACE, NMT_EDEVICE. */
 nmt_status nmt_logits(nmt_model* m, int32_t M, const float* d_t, float* d_logits, int64_t ld_logits, float* d_logZ,

@@ -567,6 +567,14 @@ __device__ __forceinline__ float gru_cell(float sr, float sz, float sni, float s
 // Row of accumulator register r for lane half h.
 __device__ __forceinline__ int acc_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
+// The larger of two floats.  With kNaN a NaN stays one (fmaxf drops it, at the
+// same price): what is made of the largest then is NaN too.
+template <bool kNaN>
+__device__ __forceinline__ float larger(float a, float b) {
+  if constexpr (kNaN) return __builtin_elementwise_maximum(a, b);
+  return fmaxf(a, b);
+}
+
 // Four floats at any 4-byte aligned address, as one access.
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 

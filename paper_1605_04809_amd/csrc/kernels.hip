@@ -1412,8 +1412,8 @@ __global__ __launch_bounds__(VocabTune<P>::VNW * 64) void k_vocab_lse(const floa
 #pragma unroll
       for (int f = 0; f < VFN; ++f)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) bm = fmaxf(bm, acc[i][f][r]);
-      const float mn = fmaxf(run_m[i], bm);
+        for (int r = 0; r < 16; ++r) bm = larger<OUT>(bm, acc[i][f][r]);
+      const float mn = larger<OUT>(run_m[i], bm);
       const bool none = mn == -INFINITY;  // nothing but masked logits so far
       const float sc = none ? 1.f : __builtin_amdgcn_exp2f((run_m[i] - mn) * kLog2e);
       const float nm = none ? 0.f : -mn * kLog2e;
@@ -1439,7 +1439,7 @@ __global__ __launch_bounds__(VocabTune<P>::VNW * 64) void k_vocab_lse(const floa
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
     const float om = __shfl_xor(run_m[i], 32, 64), os = __shfl_xor(run_s[i], 32, 64);
-    const float mx = fmaxf(run_m[i], om);
+    const float mx = larger<OUT>(run_m[i], om);
     float s = 0.f;
     if (mx != -INFINITY)
       s = run_s[i] * __builtin_amdgcn_exp2f((run_m[i] - mx) * kLog2e) +
@@ -1452,7 +1452,7 @@ __global__ __launch_bounds__(VocabTune<P>::VNW * 64) void k_vocab_lse(const floa
     const int row = m0 + rl;
     float mx = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < VNW; ++w) mx = fmaxf(mx, red[w][rl].x);
+    for (int w = 0; w < VNW; ++w) mx = larger<OUT>(mx, red[w][rl].x);
     float s = 0.f;
     if (mx != -INFINITY) {
 #pragma unroll
@@ -1712,21 +1712,23 @@ hipError_t launch_lse_combine(int B, const float2* part, int nS, const float* t,
 }
 
 // One wave per row: the slices' (max, sum) pairs merged into log Z, for a row
-// that requests nothing.
+// that requests nothing.  A NaN among its logits makes the largest NaN, and so
+// log Z; an infinite largest is log Z by itself (its sum is inf - inf).
 __global__ __launch_bounds__(256) void k_logits_lse(int M, const float2* __restrict__ part, int nS,
                                                     float* __restrict__ logZ) {
   const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (row >= M) return;
   float mx = -INFINITY;
-  for (int i = lane; i < nS; i += 64) mx = fmaxf(mx, part[(int64_t)i * M + row].x);
-  mx = wave_max(mx);
+  for (int i = lane; i < nS; i += 64) mx = larger<true>(mx, part[(int64_t)i * M + row].x);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) mx = larger<true>(mx, __shfl_xor(mx, o, 64));
   float sum = 0.f;
   for (int i = lane; i < nS; i += 64) {
     const float2 p = part[(int64_t)i * M + row];
     if (p.x != -INFINITY) sum += p.y * expf(p.x - mx);
   }
   sum = wave_sum(sum);
-  if (lane == 0) logZ[row] = mx + logf(sum);
+  if (lane == 0) logZ[row] = mx == INFINITY ? mx : mx + logf(sum);
 }
 
 hipError_t launch_logits_lse(int M, const float2* part, int nS, float* logZ, hipStream_t st) {

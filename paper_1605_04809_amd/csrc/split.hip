@@ -1102,8 +1102,8 @@ __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restr
 #pragma unroll
       for (int f = 0; f < VFN; ++f)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) bm = fmaxf(bm, acc[i][f][r]);
-      const float mn = fmaxf(run_m[i], bm);
+        for (int r = 0; r < 16; ++r) bm = larger<OUT>(bm, acc[i][f][r]);
+      const float mn = larger<OUT>(run_m[i], bm);
       const bool none = mn == -INFINITY;
       const float sc = none ? 1.f : __builtin_amdgcn_exp2f((run_m[i] - mn) * kz);
       const float nm = none ? 0.f : -mn * kz;
@@ -1128,7 +1128,7 @@ __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restr
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
     const float om = __shfl_xor(run_m[i], 32, 64), os = __shfl_xor(run_s[i], 32, 64);
-    const float mx = fmaxf(run_m[i], om);
+    const float mx = larger<OUT>(run_m[i], om);
     float s = 0.f;
     if (mx != -INFINITY)
       s = run_s[i] * __builtin_amdgcn_exp2f((run_m[i] - mx) * kz) + os * __builtin_amdgcn_exp2f((om - mx) * kz);
@@ -1139,7 +1139,7 @@ __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restr
     const int row = m0 + rl;
     float mx = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < VNW; ++w) mx = fmaxf(mx, red[w][rl].x);
+    for (int w = 0; w < VNW; ++w) mx = larger<OUT>(mx, red[w][rl].x);
     float s = 0.f;
     if (mx != -INFINITY) {
 #pragma unroll

@@ -308,3 +308,55 @@ def test_a_round_captured():
     assert nb.nmt_stream_status(run.model) == nb.NMT_OK
     w4.close()
     run.close()
+
+
+@pytest.mark.parametrize("wtype,spoil", [("f32", False), ("f32", True), ("bf16", False)])
+@pytest.mark.parametrize("V,M", [(33, 3), (515, 12), (9000, 70)])
+def test_log_sum_of_logits_that_are_not_finite(wtype, spoil, V, M):
+    """log Z is what its row's logits give: NaN beside a NaN, infinity beside
+    an infinity, and the other rows' as they are without such rows."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    rng = np.random.default_rng(V)
+    E = 100
+    model, W, b = _layer(nb, rng, E, V, wtype, spoil=spoil)
+    t = dc.round_bf16(np.tanh(rng.standard_normal((M, E))).astype(np.float32))
+    _, clean = _logits(torch, nb, model, t)
+    t[0] = np.nan                    # what nmt_step_readouts gives for an id out of range
+    t[1, 7] = np.inf
+    t[M - 1, 99] = -np.inf
+    z, lz = _logits(torch, nb, model, t)
+    want = torch.logsumexp(torch.from_numpy(z), 1).numpy()
+    assert np.isnan(lz[0]) and not np.isfinite(lz[[1, M - 1]]).any()
+    for r in (0, 1, M - 1):
+        np.testing.assert_equal(lz[r], want[r])
+    np.testing.assert_array_equal(lz[2:M - 1], clean[2:M - 1])
+    model.close()
+
+
+@pytest.mark.parametrize("wtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [70, 9000])
+def test_log_sum_beside_single_logits_that_are_not_finite(wtype, V):
+    """A bias of NaN or, with fp32 weights, of infinities in single columns (V = 9,000: of one slice alone)."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    rng = np.random.default_rng(V)
+    E = 32
+    p = {n: np.zeros(s, np.float32) for n, s in param_shapes(4, V, E, 8, 8).items()}
+    p["out_W"] = dc.round_bf16(rng.standard_normal((E, V)).astype(np.float32))
+    t = np.tanh(rng.standard_normal((5, E))).astype(np.float32)
+    infinite = ((np.inf, 40), (-np.inf, 3), (-np.inf, slice(0, 64)), (-np.inf, slice(None)))
+    for value, at in ((np.nan, 3), (np.nan, V - 1)) + (infinite if wtype == "f32" else ()):
+        p["out_b"] = np.zeros(V, np.float32)
+        p["out_b"][at] = value
+        model = nb.Model(p, 4, V, E, 8, 8, wtype)
+        z, lz = _logits(torch, nb, model, t)
+        want = torch.logsumexp(torch.from_numpy(z), 1).numpy()
+        assert np.isfinite(want).all() == (value == -np.inf and at != slice(None))
+        # (V / 256 + 256 roundings of the sum, and the result's own)
+        tol = np.where(np.isfinite(want), (V / 256 + 256) * 2.0 ** -24 + 2.0 ** -23 * np.abs(want), 0.0)
+        np.testing.assert_array_equal(np.isnan(lz), np.isnan(want))
+        with np.errstate(invalid="ignore"):
+            near = (lz == want) | np.isnan(want) | (np.abs(lz - want) <= tol)
+        assert np.all(near), (value, at)
+        model.close()
