@@ -459,7 +459,7 @@ typedef struct {
 /* Copy a 4-bit matrix to the current HIP device, laid out for the kernel.
  *   h_codes  [K x ceil(N/2)] bytes, row-major: byte i of a row holds the codes
  *            of columns 2i (low half) and 2i + 1 (high half)
- *   h_scales [ceil(K/group) x N] fp32, finite (with NMT_BF16 also once rounded)
+ *   h_scales [ceil(K/group) x N] fp32, of magnitude 2^116 or less
  *   h_zeros  [ceil(K/group) x N] bytes in [0, 15]; NULL: 8 everywhere
  *   h_bias   [N] fp32, added to every product; NULL: none
  * The caller keeps the host arrays.  Synchronous.  Errors: NMT_EINVAL, NMT_ERANGE
@@ -472,8 +472,8 @@ nmt_status nmt_w4_create(const nmt_w4_dims* dims, const uint8_t* h_codes, const 
  * scales' type, c = 8 + w / s rounded to the nearest (ties to even) within
  * [1, 15], z = 8; a group whose scale comes out 0 holds zeros.  Runs on
  * `stream` and waits for it.  Independent of the model afterwards.
- * Errors: NMT_EINVAL (also for a layer with a weight that is not finite),
- * NMT_ENOMEM, NMT_EDEVICE. */
+ * Errors: NMT_EINVAL (also for a layer with a weight that is not finite or
+ * above 7 * 2^116), NMT_ENOMEM, NMT_EDEVICE. */
 nmt_status nmt_w4_from_output(const nmt_model* m, int32_t group, int32_t stype, void* stream, nmt_w4** out);
 
 /* The matrix's sizes, and whether it has zero points of its own and a bias.

@@ -22,6 +22,7 @@
 using namespace nmt;
 
 constexpr int kW4Cols = 16, kW4Rows = 128;  // columns and rows of a packed tile
+constexpr float kMostScale = 0x1p116f;      // the largest scale that products take
 
 struct nmt_w4 {
   nmt_w4_dims dims{};
@@ -123,8 +124,7 @@ __global__ __launch_bounds__(256) void k_w4_out_scales(const void* __restrict__ 
     b_out[at.n] = b;
   }
   s_out[i] = (ST)(mx / 7.f);
-  // (a scale that rounds up to infinity is as useless as an infinite weight)
-  if (!finite || !((float)(ST)(mx / 7.f) < INFINITY)) atomicOr(bad, 1);
+  if (!finite || !(mx / 7.f <= kMostScale)) atomicOr(bad, finite ? 2 : 1);
 }
 
 // The codes under those scales, one packed vector per thread.
@@ -163,19 +163,25 @@ __global__ __launch_bounds__(256) void k_w4_out_codes(const void* __restrict__ W
 // at most 15, exact in fp16, and the inputs enter as fp16 times a power of two,
 // an fp32 input as two halves hi = fp16(x 2^e) and lo = fp16(x 2^e - hi), 22
 // bits and a sign, a bf16 input as one.  e puts the largest of a row's 128
-// inputs of a K block in [2^14, 2^15), so an input is off by at most 2^-24 of
-// itself or 2^-40 of that largest one.  A group's products are summed in fp32
-// by the MFMA, then times the scale to the block's sum and times 2^-e to the
-// row's.
+// inputs of a K block in [2^14, 2^15), so an input is off by at most 2^-23 of
+// itself (a bf16 one by nothing) or 2^-39 of that largest one.  A group's
+// products are summed in fp32 by the MFMA, then times the scale to the block's
+// sum and times 2^(14 - e) to the row's, for the codes enter as c 2^-14.  With
+// those a block's sum is below 128 * 15 * 2^15 * 2^-14 < 2^11.91 of its scales,
+// so it cannot overflow before 2^-e is taken off while the scales are at most
+// kMostScale, and 2^(14 - e) is a normal float for inputs of any size; whole
+// codes would do for scales up to 2^102 alone.  (Scales below 2^-111 lose bits
+// on the way, but fewer than the inputs' 2^-39.)
 //
 // A block takes up to RM rows, holds their inputs in LDS as MFMA fragments,
 // converted once a block (K too long for LDS is taken in chunks), and walks over
 // the column tiles, one for each group of WK waves at a time.  The codes stream
 // from memory straight into registers, D K blocks ahead and from before the
 // inputs are converted, each 16-byte vector the operand of four MFMA steps of
-// 32 rows of W: 9 instructions turn a 32-bit word into eight fp16 values
-// (0x6400 | n is 1024 + n; the upper nibble of a byte, in place, gives
-// 1024 + 16 n).  Lane 16 q + r holds column r of a tile, so it needs one scale
+// 32 rows of W: 9 instructions turn a 32-bit word into eight fp16 values (the
+// old way of making floats of small whole numbers, by putting them into the
+// last bits of a known one: 0x2c00 | n is 2^-4 + n 2^-14; the upper nibble of a
+// byte, in place, gives 2^-4 + n 2^-10).  Lane 16 q + r holds column r of a tile, so it needs one scale
 // and one zero point a group.  WK > 1 splits K between waves where there are
 // few columns; their sums meet in LDS in a fixed order.
 //
@@ -214,11 +220,11 @@ struct W4Shape {
 constexpr int w4_waves(int RM, bool long_k) { return RM > 16 || (RM == 16 && long_k) ? 16 : 8; }
 constexpr int w4_depth(int RM, int W, int GPB) { return W > 8 || (RM == 16 && GPB == 4) ? 2 : 4; }
 
-// Eight codes of a word as fp16, minus the zero point: zl = -(1024 + z) and
-// zh = -(64 + z), twice each.  (The masks sit in registers, or the compiler
+// Eight codes of a word as fp16, minus the zero point, times 2^-14: zl = -(2^-4
+// + z 2^-14) and zh = -(2^-8 + z 2^-14), twice each.  (The masks sit in registers, or the compiler
 // splits each and-or for the sake of its literals.)
 struct Masks {
-  uint32_t lo = 0x000f000fu, hi = 0x00f000f0u, base = 0x64006400u;
+  uint32_t lo = 0x000f000fu, hi = 0x00f000f0u, base = 0x2c002c00u;
   __device__ __forceinline__ Masks() { asm("" : "+s"(lo), "+s"(hi), "+v"(base)); }
 };
 __device__ __forceinline__ f16x8 codes_f16(uint32_t w, f16x2 zl, f16x2 zh, const Masks& k) {
@@ -284,7 +290,7 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(4))) voi
   // [K block][step][part][lane quarter][row ^ (4 step + quarter)] fragments
   // (rows permuted within their tile, so that the 16 lanes that write one
   // row's vectors do not meet in one bank; RM = 4 keeps them in order), then
-  // [K block][16 RT] 2^-e, then the K shares' sums
+  // [K block][16 RT] 2^(14 - e), then the K shares' sums
   extern __shared__ f32x4 lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, q = lane >> 4;
@@ -320,7 +326,7 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(4))) voi
 #pragma unroll
   for (int d = 0; d < D; ++d) load(ring[d], tile, d * sh.wk + wk);
 
-  // Eight inputs of a K block that 16 lanes hold to LDS; returns the block's 2^-e
+  // Eight inputs of a K block that 16 lanes hold to LDS; returns the block's 2^(14 - e)
   auto convert = [&](const float (&v)[8], f32x4* to) {
     constexpr uint32_t kInf = 0x7f800000u;
     uint32_t mx = largest16(v);  // (a NaN makes all of its row's outputs NaN, at any scale)
@@ -346,7 +352,7 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(4))) voi
         for (int e = 0; e < 8; ++e) lo[e] = fabsf(v[e]) < INFINITY ? lo[e] : (_Float16)0.f;
     to[0] = __builtin_bit_cast(f32x4, hi);
     if constexpr (HV == 2) to[4 * RM] = __builtin_bit_cast(f32x4, lo);
-    return __builtin_amdgcn_ldexpf(1.f, -e2);
+    return __builtin_amdgcn_ldexpf(1.f, 14 - e2);
   };
   // K blocks kb0 .. kb0 + nkb - 1 of the rows to LDS: 16 lanes take one of a
   // row, U of them at a time so that their loads are in flight together
@@ -403,10 +409,10 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(4))) voi
       const bool first = s % kStepsPerGroup == 0;
       const int g = s / kStepsPerGroup;
       if (s < 3) fetch(s + 1);
-      // the group's zero point in both halves; -(1024 + z) and -(64 + z) as bits
+      // the group's zero point in both halves, and zl and zh as bits
       const uint32_t z = __builtin_amdgcn_perm(0u, zeros4, 0x0c000c00u | (uint32_t)g * 0x00010001u);
-      const f16x2 zl = __builtin_bit_cast(f16x2, z | 0xe400e400u);
-      const f16x2 zh = __builtin_bit_cast(f16x2, (z << 4) | 0xd400d400u);
+      const f16x2 zl = __builtin_bit_cast(f16x2, z | 0xac00ac00u);
+      const f16x2 zh = __builtin_bit_cast(f16x2, (z << 4) | 0x9c009c00u);
       const uint32_t w = s == 0 ? b.code.x : s == 1 ? b.code.y : s == 2 ? b.code.z : b.code.w;
       const f16x8 c = codes_f16(w, zl, zh, masks);
 #pragma unroll
@@ -602,10 +608,8 @@ nmt_status nmt_w4_create(const nmt_w4_dims* dims, const uint8_t* h_codes, const 
   if (d.group < 32 || d.group % 32) return entry_fail(NMT_EINVAL, "group must be a positive multiple of 32");
   if (!known_type(d.stype)) return entry_fail(NMT_EINVAL, "unknown type of scales");
   const size_t ng = (size_t)ceil_div(d.K, d.group) * d.N, nc = (size_t)d.K * (((size_t)d.N + 1) / 2);
-  // the largest fp32 below what rounds to a bf16 infinity
-  const float most = d.stype == NMT_BF16 ? 0x1.fefffep127f : 0x1.fffffep127f;
   for (size_t i = 0; i < ng; ++i)
-    if (!(std::fabs(h_scales[i]) <= most)) return entry_fail(NMT_EINVAL, "a scale is not finite in the scales' type");
+    if (!(std::fabs(h_scales[i]) <= kMostScale)) return entry_fail(NMT_EINVAL, "a scale is NaN or above 2^116");
   if (h_zeros)
     for (size_t i = 0; i < ng; ++i)
       if (h_zeros[i] > 15) return entry_fail(NMT_ERANGE, "a zero point is above 15");
@@ -685,7 +689,8 @@ nmt_status nmt_w4_from_output(const nmt_model* m, int32_t group, int32_t stype, 
   if (e != hipSuccess || h_bad) {
     nmt_w4_destroy(w);
     return e != hipSuccess ? entry_hip_fail(e, "nmt_w4_from_output")
-                           : entry_fail(NMT_EINVAL, "the model's output layer has a weight that is not finite");
+           : h_bad & 1     ? entry_fail(NMT_EINVAL, "the model's output layer has a weight that is not finite")
+                           : entry_fail(NMT_EINVAL, "the model's output layer has a weight above 7 * 2^116");
   }
   *out = w;
   return entry_ok();

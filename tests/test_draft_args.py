@@ -96,3 +96,12 @@ def test_what_a_round_emits_is_distributed_as_the_target(certain):
                 first[nxt[0]] += (~kept).mean() / n
         got += weight * first
     assert np.abs(got - p).max() <= 2.0 * V / n
+
+
+@pytest.mark.parametrize("value", [2.0 ** 116 * (1 + 2.0 ** -23), -1e35, 3e38])
+@pytest.mark.parametrize("stype", [0, 1])
+def test_w4_create_refuses_scales_that_products_do_not_take(value, stype):
+    s = np.ones((2, 7), np.float32)
+    s[0, 3] = value
+    assert _create(scales=s, stype=stype) == nb.NMT_EINVAL
+    assert "scale" in nb.last_error()

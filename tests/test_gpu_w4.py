@@ -364,3 +364,57 @@ def test_more_rows_than_a_launch_takes():
     nb.nmt_w4_product(w, few, want)
     assert torch.equal(y[at], want) and bool(torch.isfinite(y).all())
     w.close()
+
+
+@pytest.mark.parametrize("xt", ["f32", "bf16"])
+@pytest.mark.parametrize("K,M,group", [(40, 3, 32), (300, 20, 32), (300, 40, 128), (7000, 3, 64)])
+def test_scales_of_any_size(xt, K, M, group):
+    """Columns with scales from 2^-100 to nearly 2^116 under rows whose products are ordinary: finite wherever
+    fp32 holds the sum, each within the bound of its own size."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    rng = np.random.default_rng(12)
+    N = 70
+    c = dc.make_w4(rng, K, N, group, True, False)
+    e = rng.integers(-100, 116, size=N)
+    e[:6] = [115, 115, 110, 106, 102, -100]
+    unit = np.exp2(np.floor(np.log2(np.abs(c["scales"]).max(0))))
+    c["scales"] = (c["scales"] / unit * np.exp2(e)).astype(np.float32)   # the largest of a column in [2^e, 2^(e + 1))
+    zero = c["zeros"].astype(np.float64)[np.arange(K) // group]
+    c["w"] = c["scales"].astype(np.float64)[np.arange(K) // group] * (c["codes"].astype(np.float64) - zero)
+    w = _handle(nb, c, K, N, group)
+    x = rng.standard_normal((M, K)) * np.exp2(rng.integers(-100, 12, size=M))[:, None]
+    x[0] *= np.exp2(-20 - np.log2(np.abs(x[0]).max()))      # tiny beside the largest scales
+    x[1] *= np.exp2(1 - np.log2(np.abs(x[1]).max()))        # ordinary ones
+    x = x.astype(np.float32)
+    x = dc.round_bf16(x) if xt == "bf16" else x
+    y = torch.zeros((M, N), device="cuda")
+    nb.nmt_w4_product(w, _rows(torch, x, getattr(torch, TYPES[xt]))[0], y)
+    got = y.cpu().numpy().astype(np.float64)
+    a, aw = np.abs(x.astype(np.float64)), np.abs(c["w"])
+    # a term of sum |x||w| below half of fp32's largest value cannot make any partial sum infinite
+    holds = a @ aw < 2.0 ** 127
+    assert holds[0].all() and holds[1, 5:].any() and np.isfinite(got[holds]).all()
+    bound = dc.w4_bound(x, c, K, group, "f32", None)
+    worst = np.max((np.abs(got - x.astype(np.float64) @ c["w"]) / bound)[holds])
+    print(f"K={K} M={M} group={group} {xt}: error {worst:.3f} of the bound", flush=True)
+    assert worst <= 1.0
+    w.close()
+
+
+
+def test_output_layers_too_large_for_scales():
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    wl = make_workload(CONFIGS["tiny"].replace(seed=12))
+    for value, ok in ((-7.0 * 2.0 ** 116, True), (7.5 * 2.0 ** 116, False)):
+        wl.params["out_W"][1, 2] = value
+        model = nb.Model.from_workload(wl)
+        for stype in ("f32", "bf16"):
+            if ok:
+                nb.W4.from_output(model, 32, stype).close()
+                continue
+            with pytest.raises(nb.NmtError, match="above") as ei:
+                nb.W4.from_output(model, 32, stype)
+            assert ei.value.status == nb.NMT_EINVAL
+        model.close()
