@@ -484,9 +484,11 @@ nmt_status nmt_w4_info(const nmt_w4* w, nmt_w4_dims* dims, int32_t* has_zeros, i
  *   d_x   row i at x + i * ld_x elements of x_type, K values (ld_x >= K)
  *   d_y   out: row i at y + i * ld_y elements of y_type, N values (ld_y >= N;
  *         what lies between rows is not written); must not overlap x
- * Products and sums are fp32 (fp32 inputs enter with 22 significant bits or
- * more, relative to the largest of each 128 inputs); bf16 outputs are rounded
- * once, nearest even.  Infinities and NaN in x reach the row's outputs as in
+ * Products and sums are fp32.  Inputs enter the matrix cores in fp16, fp32 ones
+ * as two halves: an fp32 input is off by at most 2^-23 of itself, a bf16 one by
+ * nothing, or either by 2^-39 of the largest of its 128 (inputs 128 i to
+ * 128 i + 127 of the row) where that is more.  bf16 outputs are rounded once,
+ * nearest even.  Infinities and NaN in x reach the row's outputs as in
  * fp32 products.  Pointers need their element's alignment only (16-byte
  * aligned rows are read and written faster).  Rows are independent: a row's
  * outputs do not depend on the others' values.  M = 0 is a no-op; the call

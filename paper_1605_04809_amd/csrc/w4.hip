@@ -337,8 +337,9 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(4))) voi
       for (int e = 0; e < 8; ++e) w[e] = fabsf(v[e]) < INFINITY ? v[e] : 0.f;
       mx = largest16(w);
     }
-    // 2^e puts the largest in [2^14, 2^15); e not above 120, so that 2^-e is normal
-    const int e2 = mx - 1 < kInf - 1 ? min(15 - __builtin_amdgcn_frexp_expf(__builtin_bit_cast(float, mx)), 120) : 0;
+    // 2^e puts the largest in [2^14, 2^15); e not above 127, so that 2^e is finite (at 127 the halves still
+    // hold every bit of fp32's smallest values, whose steps are 2^-149)
+    const int e2 = mx - 1 < kInf - 1 ? min(15 - __builtin_amdgcn_frexp_expf(__builtin_bit_cast(float, mx)), 127) : 0;
     const float up = __builtin_amdgcn_ldexpf(1.f, e2);
     f16x8 hi, lo;
 #pragma unroll

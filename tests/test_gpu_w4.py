@@ -418,3 +418,26 @@ def test_output_layers_too_large_for_scales():
                 nb.W4.from_output(model, 32, stype)
             assert ei.value.status == nb.NMT_EINVAL
         model.close()
+
+
+@pytest.mark.parametrize("K,M", [(40, 3), (300, 20), (300, 40), (7000, 3)])
+def test_the_smallest_inputs(K, M):
+    """Rows of fp32's smallest values (steps of 2^-149), under scales that bring their products back to ordinary
+    size: every bit of them counts."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    rng = np.random.default_rng(13)
+    N, group = 50, 64
+    c = dc.make_w4(rng, K, N, group, True, False)
+    for k in ("scales", "w"):
+        c[k] = (c[k] * 2.0 ** 100).astype(c[k].dtype)
+    w = _handle(nb, c, K, N, group)
+    step = np.exp2(rng.integers(0, 22, size=M))[:, None]
+    step[:2] = [[1.0], [2.0]]
+    x = (np.rint(rng.standard_normal((M, K)) * step) * 2.0 ** -149).astype(np.float32)
+    x[0, 0], x[1, K - 1] = 2.0 ** -149, -(2.0 ** -148)
+    y = torch.zeros((M, N), device="cuda")
+    nb.nmt_w4_product(w, torch.from_numpy(x).cuda(), y)
+    got, want = y.cpu().numpy().astype(np.float64), x.astype(np.float64) @ c["w"]
+    assert np.all(np.abs(got - want) <= dc.w4_bound(x, c, K, group, "f32", want))
+    w.close()
