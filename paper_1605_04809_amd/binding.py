@@ -253,6 +253,18 @@ def _checked(t, dtype, n: int, what: str):
     return _ptr(t)
 
 
+def _workspace(nbytes: int, stream):
+    """Scratch for one call on `stream` (None: the current one), from that
+    stream's own pool: it goes back there when the call has been queued, so
+    that whoever gets it next works behind the call."""
+    import torch
+    empty = lambda: torch.empty(max(nbytes, 256), dtype=torch.uint8, device="cuda")
+    if stream is None:
+        return empty()
+    with torch.cuda.stream(stream):
+        return empty()
+
+
 def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream.cuda_stream
@@ -393,11 +405,10 @@ def nmt_score_batch(model: Model, src: Source, s_prev, y_prev, sent_id, req, log
     With any of ``alpha``, ``c``, ``s1``, ``t`` given, nmt_score_batch_debug is
     called and those intermediates are written too.
     """
-    import torch
     lib = load_library()
     B = int(y_prev.shape[0])
     if workspace is None:
-        workspace = torch.empty(max(nmt_score_workspace_bytes(model, B), 256), dtype=torch.uint8, device="cuda")
+        workspace = _workspace(nmt_score_workspace_bytes(model, B), stream)
     args = [model.handle, src.handle, B, _ptr(s_prev), _ptr(y_prev), _ptr(sent_id), _ptr(req), _ptr(logp),
             _ptr(s_new), _ptr(logZ), _ptr(workspace), workspace.numel(), _stream(stream)]
     if any(x is not None for x in (alpha, c, s1, t)):
@@ -440,11 +451,10 @@ def nmt_ensemble_workspace_bytes(models, B: int) -> int:
 def nmt_score_ensemble(models, srcs, s_prev, y_prev, sent_id, req, logp, s_new, logZ=None, weights=None,
                        score=None, workspace=None, stream=None):
     """One batched step of the same rows under K models; logp is [K, B]."""
-    import torch
     lib = load_library()
     K, B = len(models), int(y_prev.shape[0])
     if workspace is None:
-        workspace = torch.empty(max(nmt_ensemble_workspace_bytes(models, B), 256), dtype=torch.uint8, device="cuda")
+        workspace = _workspace(nmt_ensemble_workspace_bytes(models, B), stream)
     sp = (_VP * K)(*[_ptr(x) for x in s_prev])
     sn = (_VP * K)(*[_ptr(x) for x in s_new])
     w = None if weights is None else (ctypes.c_float * K)(*[float(x) for x in weights])
@@ -474,11 +484,10 @@ def nmt_profile_end(model: Model, stream=None) -> dict:
 def nmt_score_forest_step(model: Model, src: Source, state_pool, state_row, y_prev, sent_id, req_off, req, logp,
                           s_new, logZ=None, workspace=None, stream=None):
     """One ScoreBatch level: gathered input states, CSR requests (see nmt.h)."""
-    import torch
     lib = load_library()
     B = int(y_prev.shape[0])
     if workspace is None:
-        workspace = torch.empty(max(nmt_score_workspace_bytes(model, B), 256), dtype=torch.uint8, device="cuda")
+        workspace = _workspace(nmt_score_workspace_bytes(model, B), stream)
     _check(lib.nmt_score_forest_step(model.handle, src.handle, B, _ptr(state_pool), int(state_pool.shape[0]),
                                      _ptr(state_row), _ptr(y_prev), _ptr(sent_id), _ptr(req_off), _ptr(req),
                                      int(req.shape[0]), _ptr(logp), _ptr(s_new), _ptr(logZ), _ptr(workspace),
@@ -555,7 +564,7 @@ def nmt_step_readouts(model: Model, src: Source, state_pool, y_prev, sent_id, s_
     import torch
     B = int(y_prev.shape[0])
     if workspace is None:
-        workspace = torch.empty(max(nmt_score_workspace_bytes(model, B), 256), dtype=torch.uint8, device="cuda")
+        workspace = _workspace(nmt_score_workspace_bytes(model, B), stream)
     _check(load_library().nmt_step_readouts(
         model.handle, src.handle, B, _ptr(state_pool), int(state_pool.shape[0]),
         _checked(state_row, torch.int32, B, "state_row"), _checked(y_prev, torch.int32, B, "y_prev"),
@@ -568,7 +577,7 @@ def nmt_logits(model: Model, t, logits, logZ=None, workspace=None, stream=None):
     import torch
     M = int(t.shape[0])
     if workspace is None:
-        workspace = torch.empty(max(nmt_score_workspace_bytes(model, M), 256), dtype=torch.uint8, device="cuda")
+        workspace = _workspace(nmt_score_workspace_bytes(model, M), stream)
     zp, zt, zl = _rows(logits, model.V, M)
     if zt != NMT_F32:
         raise ValueError("logits must be fp32")
@@ -588,7 +597,7 @@ def nmt_verify_drafts(model: Model, draft_off, draft, target, proposal, u, accep
     import torch
     S, n, i32, f32 = int(draft_off.shape[0]) - 1, int(draft.shape[0]), torch.int32, torch.float32
     if workspace is None:
-        workspace = torch.empty(max(nmt_verify_workspace_bytes(model, S, n), 256), dtype=torch.uint8, device="cuda")
+        workspace = _workspace(nmt_verify_workspace_bytes(model, S, n), stream)
     tp, tt, tl = _rows(target, model.V, n + S)
     pp, pt, pl = (None, NMT_F32, 0) if proposal is None or n == 0 else _rows(proposal, model.V, n)
     _check(load_library().nmt_verify_drafts(
@@ -665,11 +674,9 @@ def nmt_forest_workspace_bytes(model: Model, forest: Forest) -> int:
 def nmt_score_forest(model: Model, src: Source, forest: Forest, hyp_states, pair_logp, req_logp=None,
                      node_states=None, workspace=None, stream=None):
     """ScoreBatch on the device: per-pair log p(phrase | hypothesis)."""
-    import torch
     lib = load_library()
     if workspace is None:
-        workspace = torch.empty(max(nmt_forest_workspace_bytes(model, forest), 256), dtype=torch.uint8,
-                                device="cuda")
+        workspace = _workspace(nmt_forest_workspace_bytes(model, forest), stream)
     _check(lib.nmt_score_forest(model.handle, src.handle, forest.handle, _ptr(hyp_states), _ptr(pair_logp),
                                 _ptr(req_logp), _ptr(node_states), _ptr(workspace), workspace.numel(),
                                 _stream(stream)))

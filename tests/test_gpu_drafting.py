@@ -360,3 +360,47 @@ def test_log_sum_beside_single_logits_that_are_not_finite(wtype, V):
             near = (lz == want) | np.isnan(want) | (np.abs(lz - want) <= tol)
         assert np.all(near), (value, at)
         model.close()
+
+
+@pytest.mark.parametrize("call", ["score", "forest_step", "ensemble", "readouts", "logits", "verify"])
+def test_scratch_of_a_call_on_another_stream(call):
+    """A call on a stream that is not the current one, with no workspace given: memory that the current stream
+    gets while the call waits its turn there is not the call's scratch."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    wl = make_workload(CONFIGS["tiny"].replace(S=4, B=4, V=3000, seed=35))
+    run, c = GpuRun(wl), wl.cfg
+    i32, B = dict(dtype=torch.int32, device="cuda"), wl.cfg.B
+    sp, y, sent, req = cuda(wl.s_prev), cuda(wl.y_prev), cuda(wl.sent_id), cuda(wl.req)
+    logp, s_new, t = torch.empty(B, device="cuda"), torch.empty((B, c.H), device="cuda"), torch.zeros((B, c.E), device="cuda")
+    z, logZ = torch.zeros((B, c.V), device="cuda"), torch.empty(B, device="cuda")
+    rows, off, at0 = torch.arange(B, **i32), torch.arange(B + 1, **i32), torch.zeros(B + 1, **i32)
+    u, acc, nxt = torch.full((B,), 0.5, device="cuda"), torch.empty(B, **i32), torch.empty(B, **i32)
+    need = nb.nmt_score_workspace_bytes(run.model, B)
+    need, go = {
+        "score": (need, lambda s: nb.nmt_score_batch(run.model, run.src, sp, y, sent, req, logp, s_new, stream=s)),
+        "forest_step": (need, lambda s: nb.nmt_score_forest_step(run.model, run.src, sp, rows, y, sent, off, req, logp,
+                                                                 s_new, stream=s)),
+        "ensemble": (nb.nmt_ensemble_workspace_bytes([run.model], B),
+                     lambda s: nb.nmt_score_ensemble([run.model], [run.src], [sp], y, sent, req, logp[None], [s_new],
+                                                     stream=s)),
+        "readouts": (need, lambda s: nb.nmt_step_readouts(run.model, run.src, sp, y, sent, s_new, t, stream=s)),
+        "logits": (need, lambda s: nb.nmt_logits(run.model, t, z, logZ=logZ, stream=s)),
+        "verify": (nb.nmt_verify_workspace_bytes(run.model, B, 0),
+                   lambda s: nb.nmt_verify_drafts(run.model, at0, at0[:0], z, None, u, acc, nxt, stream=s)),
+    }[call]
+    a = torch.zeros((4096, 4096), device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(200):     # over 0.1 s, far longer than what follows takes on the host
+            a = a @ a
+    go(s)
+    theirs = [torch.full((max(need, 256),), 7, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.current_stream().synchronize()
+    assert not s.query()         # the call still waits
+    s.synchronize()
+    assert all(bool((x == 7).all()) for x in theirs)
+    assert nb.nmt_stream_status(run.model) == nb.NMT_OK
+    run.close()
