@@ -434,7 +434,11 @@ nmt_status nmt_step_readouts(nmt_model* m, const nmt_source* src, int32_t B, con
 /* The logits of every next word of M readouts: z = t out_W + out_b.
  *   d_t [M x E]       readouts (any fp32 values; a bf16 model rounds them to
  *                     bf16, nearest even).  A row that holds an infinity or a
- *                     NaN gets logits that are not finite.
+ *                     NaN gets logits that are not finite.  With fp32 weights
+ *                     the products may take both factors in two fp16 halves
+ *                     each: a readout is off by at most 2^-23 of itself or 2^-39
+ *                     of its row's largest, a weight by 2^-23 of itself or 2^-25
+ *                     of its column's largest.
  *   d_logits          out: row i at d_logits + i * ld_logits, V fp32 values
  *                     (ld_logits >= V; what lies between rows is not written)
  *   d_logZ [M]        out, nullable: log sum_v exp(z_v); NaN where a logit is, else

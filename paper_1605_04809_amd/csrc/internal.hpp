@@ -298,7 +298,7 @@ struct SpA {
   float most, least;
 };
 constexpr int kSplitReadout = 14;  // activations' scale: tanh readouts (at most 1)
-constexpr int kSplitBiasRoom = 24;
+constexpr int kSplitBiasRoom = 127;  // (2^127 is finite, and takes fp32's smallest normal value to 2)
 // states and annotations (at most 1 from the model; a row whose largest is in [2^-12, 16) stays on the halves)
 constexpr int kSplitState = 12;
 constexpr int kSpLongK = 256;      // K from which the tile GEMM splits K between wave groups

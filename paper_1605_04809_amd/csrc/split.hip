@@ -841,10 +841,11 @@ constexpr int kSvVectors = 9216;  // LDS vectors of the activation tile (144 KB)
 
 // OUT: the kernel of nmt_logits, which also writes each logit to zout (row
 // stride ldz) and takes readouts of any magnitude: a row is scaled by the
-// power of two that puts its largest in [2^14, 2^15), as far as its bias has
-// room in the accumulators, so it keeps 22 bits whatever its size (a tanh
-// readout's row has the fixed scale's values but for that power of two), and
-// its logits are folded in natural units.  The stores are 16 bytes a lane, a
+// power of two that puts its largest in [2^14, 2^15), as far as the bias has
+// room in the accumulators (where it ends, what is lost is below 2^-130 of the
+// largest bias), so it keeps 22 bits whatever its size (a tanh readout's row has
+// the fixed scale's values but for that power of two), and its logits are
+// folded in natural units.  The stores are 16 bytes a lane, a
 // 128-byte line of a row per column block over four instructions.
 template <int VPF, int VTM, bool OUT = false>
 __global__ __launch_bounds__(kSvWaves * 64) void k_vocab_sp(const float* __restrict__ t, int M, int E, int NK,

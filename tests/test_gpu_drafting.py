@@ -404,3 +404,24 @@ def test_scratch_of_a_call_on_another_stream(call):
     assert all(bool((x == 7).all()) for x in theirs)
     assert nb.nmt_stream_status(run.model) == nb.NMT_OK
     run.close()
+
+
+@pytest.mark.parametrize("wtype,spoil", [("f32", False), ("f32", True), ("bf16", False)])
+def test_logits_of_small_rows(wtype, spoil):
+    """Without a bias a row of any size keeps its own digits: relative to sum |t||W|, and where it is
+    fp32's smallest values that count, 2^-150 for each rounding."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    rng = np.random.default_rng(11)
+    E, V = 100, 515
+    model, W, b = _layer(nb, rng, E, V, wtype, bias=0.0, spoil=spoil)
+    exps = [-24, -25, -40, -64, -80, -100] + ([-124, -135, -140] if wtype == "f32" and not spoil else [])
+    t = np.stack([rng.standard_normal(E) * 2.0 ** e for e in exps]).astype(np.float32)
+    t = dc.round_bf16(t) if wtype == "bf16" else t
+    z, _ = _logits(torch, nb, model, t)
+    t64 = t.astype(np.float64)
+    bound = (E + 16) * 2.0 ** -24 * (np.abs(t64) @ np.abs(W)) + (E + 16) * 2.0 ** -150
+    worst = np.max(np.abs(z - t64 @ W) / bound, axis=1)
+    print(wtype, spoil, worst, flush=True)
+    assert np.all(worst <= 1.0)
+    model.close()
