@@ -560,13 +560,15 @@ def nmt_w4_product(w: W4, x, y, stream=None):
 
 def nmt_step_readouts(model: Model, src: Source, state_pool, y_prev, sent_id, s_new, t, state_row=None,
                       workspace=None, stream=None):
-    """One step without the vocabulary: new states and readouts t [B, E] (see nmt.h)."""
+    """One step without the vocabulary, from states state_pool [rows, H]: new states and readouts t [B, E] (see
+    nmt.h)."""
     import torch
-    B = int(y_prev.shape[0])
+    B, pool_rows = int(y_prev.shape[0]), int(state_pool.shape[0])
+    pool = _checked(state_pool, torch.float32, pool_rows * model.H, "state_pool")
     if workspace is None:
         workspace = _workspace(nmt_score_workspace_bytes(model, B), stream)
     _check(load_library().nmt_step_readouts(
-        model.handle, src.handle, B, _ptr(state_pool), int(state_pool.shape[0]),
+        model.handle, src.handle, B, pool, pool_rows,
         _checked(state_row, torch.int32, B, "state_row"), _checked(y_prev, torch.int32, B, "y_prev"),
         _checked(sent_id, torch.int32, B, "sent_id"), _checked(s_new, torch.float32, B * model.H, "s_new"),
         _checked(t, torch.float32, B * model.E, "t"), _ptr(workspace), workspace.numel(), _stream(stream)))

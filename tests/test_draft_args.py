@@ -2,6 +2,7 @@
 the 64-bit verification that the GPU tests compare with against what it is
 meant to do: the words that a round emits are distributed as the target's."""
 import ctypes
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -105,3 +106,13 @@ def test_w4_create_refuses_scales_that_products_do_not_take(value, stype):
     s[0, 3] = value
     assert _create(scales=s, stype=stype) == nb.NMT_EINVAL
     assert "scale" in nb.last_error()
+
+
+@pytest.mark.parametrize("shape,dtype", [((4, 63), "float32"), ((4, 64), "float64"), ((4, 64), "bfloat16"),
+                                         ((256,), "float32")])
+def test_readouts_refuse_a_pool_of_other_states(shape, dtype):
+    """Before anything else: such a pool's rows would be read beyond its end."""
+    torch = pytest.importorskip("torch")
+    pool, y = torch.zeros(shape, dtype=getattr(torch, dtype)), torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError, match="state_pool"):
+        nb.nmt_step_readouts(SimpleNamespace(H=64, E=32), None, pool, y, y, None, None)
