@@ -512,9 +512,12 @@ class W4:
 
     @staticmethod
     def _host(a, dtype, shape, what):
-        a = np.ascontiguousarray(a, dtype=dtype)
+        given = np.asarray(a)
+        a = np.ascontiguousarray(given, dtype=dtype)
         if a.shape != shape:
             raise ValueError(f"{what}: expected shape {shape}, got {a.shape}")
+        if dtype == np.uint8 and given.dtype.itemsize > 1 and not np.array_equal(a, given):
+            raise ValueError(f"{what}: expected bytes, got {given.dtype} with other values")
         return a
 
     @classmethod

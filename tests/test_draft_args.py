@@ -116,3 +116,23 @@ def test_readouts_refuse_a_pool_of_other_states(shape, dtype):
     pool, y = torch.zeros(shape, dtype=getattr(torch, dtype)), torch.zeros(4, dtype=torch.int32)
     with pytest.raises(ValueError, match="state_pool"):
         nb.nmt_step_readouts(SimpleNamespace(H=64, E=32), None, pool, y, y, None, None)
+
+
+@pytest.mark.parametrize("what,value", [("codes", 256 + 3), ("codes", -1), ("codes", 2.5), ("zeros", 256 + 8),
+                                        ("zeros", 7.5)])
+def test_codes_and_zero_points_that_are_no_bytes(what, value):
+    """Refused, not taken modulo 256 or cut off."""
+    a = {"codes": np.zeros((4, 2), np.float64), "zeros": np.full((1, 4), 8.0)}
+    a[what][0, 1] = value
+    if value == int(value):
+        a = {k: v.astype(np.int64) for k, v in a.items()}
+    with pytest.raises(ValueError, match=what):
+        nb.W4(a["codes"], np.ones((1, 4), np.float32), 4, 4, 32, zeros=a["zeros"])
+
+
+def test_codes_of_a_wider_type_that_are_bytes():
+    """The same as bytes: what is refused here is a zero point above 15, by the library."""
+    z = np.full((1, 4), 16, np.int64)
+    with pytest.raises(nb.NmtError) as ei:
+        nb.W4(np.full((4, 2), 255, np.int32), np.ones((1, 4)), 4, 4, 32, zeros=z)
+    assert ei.value.status == nb.NMT_ERANGE
