@@ -1727,7 +1727,7 @@ nmt_status entry_fail(nmt_status st, const char* msg) { return fail(st, "%s", ms
 nmt_status entry_hip_fail(hipError_t e, const char* what) { return hip_fail(e, what); }
 nmt_status entry_ok() { return ok(); }
 nmt_status entry_check_device(const nmt_model* m) { return check_device(m); }
-OutputLayer output_layer(const nmt_model* m) { return OutputLayer{&m->out, m->dims.E, m->dims.V, m->device}; }
+OutputLayer output_layer(const nmt_model* m) { return OutputLayer{&m->out, m->dims.E, m->dims.V, m->cus}; }
 int* error_flag(nmt_model* m) { return m->err; }
 }  // namespace nmt
 

@@ -14,11 +14,12 @@ nmt_status entry_ok();
 // NMT_EINVAL unless the model's device is the current one.
 nmt_status entry_check_device(const nmt_model* m);
 
-// A model's packed output weights, and its device error flag (bit 0: an id
-// out of range, bit 1: a row of logits that is no distribution).
+// A model's packed output weights and its device's compute units, and its
+// device error flag (bit 0: an id out of range, bit 1: a row of logits that is
+// no distribution).
 struct OutputLayer {
   const Packed* W;
-  int E, V, device;
+  int E, V, cus;
 };
 OutputLayer output_layer(const nmt_model* m);
 int* error_flag(nmt_model* m);

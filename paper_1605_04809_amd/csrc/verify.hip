@@ -42,7 +42,6 @@ constexpr int kUnit = 512;        // words whose residual one wave sums at a tim
 constexpr int kFinish = 8;        // waves a block that judges long rows ...
 constexpr int kJudge = 16;        // ... and positions it judges at a time, 16 lanes a row
 constexpr int kSmall = 8;         // positions that a block of the one-launch form judges at a time
-constexpr int kCUs = 256;
 
 // A row's (or a part's) largest logit and the sum of e^(z - max).  A NaN makes
 // the max NaN, and a row of nothing but -infinity has max -infinity and sum 0.
@@ -697,7 +696,8 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   auto bad_type = [](int32_t t) { return t != NMT_F32 && t != NMT_BF16; };
   if (bad_type(target_type) || (d_proposal && bad_type(proposal_type)))
     return entry_fail(NMT_EINVAL, "unknown element type");
-  const int V = output_layer(m).V;
+  const OutputLayer layer = output_layer(m);
+  const int V = layer.V, cus = layer.cus;
   if (ld_target < V || (d_proposal && ld_proposal < V)) return entry_fail(NMT_EINVAL, "a row stride is below V");
   if (((uintptr_t)d_target & (target_type == NMT_BF16 ? 1 : 3)) ||
       ((uintptr_t)d_proposal & (proposal_type == NMT_BF16 ? 1 : 3)))
@@ -706,7 +706,7 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   // (V = 1,000: 8.4 us against 11.1 in two launches for one sequence, 16.4
   // against 15.4 for 512; V = 4,000 and one sequence: 13.8 against 11.5), and
   // for rows too short for the other form's loads.
-  const bool small = V < 8 || (V <= kWavePart && S <= kCUs);
+  const bool small = V < 8 || (V <= kWavePart && S <= cus);
   // Parts as long as the grid still gives each CU four blocks (parts four times
   // as long measured the same), and blocks of a sequence's residual until every
   // wave has one unit or each CU two blocks: each judges its sequence by itself
@@ -714,10 +714,10 @@ nmt_status nmt_verify_drafts(nmt_model* m, int32_t S, int32_t n_draft, const int
   // 39.5 with twice as many blocks of four waves).
   const int64_t n_rows = (int64_t)n_draft + S + (d_proposal ? n_draft : 0);
   int part_len = kWaves * kWavePart;
-  while (part_len > kLeastPart && n_rows * ceil_div(V, part_len) < 4 * kCUs) part_len /= 2;
+  while (part_len > kLeastPart && n_rows * ceil_div(V, part_len) < 4 * cus) part_len /= 2;
   const int parts = ceil_div(V, part_len), units = ceil_div(V, kUnit);
   const int64_t n_parts = n_rows * parts;
-  const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, kFinish), 2 * kCUs / S));
+  const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, kFinish), 2 * cus / S));
   // a launch's threads are counted in 32 bits
   if (S >= (1 << 22) || n_parts >= (1 << 24))
     return entry_fail(NMT_EINVAL, "too many rows of logits for one call");
