@@ -535,7 +535,9 @@ size_t nmt_verify_workspace_bytes(const nmt_model* m, int32_t S, int32_t n_draft
  *   d_draft_logp [n_draft]  out, nullable: log p_j(d_j) of every draft, kept
  *                      or not (NaN where the draft or the row is no good)
  *   d_next_logp [S]    out, nullable: log p_a of d_next
- * Sums and comparisons are in 64 bits.  Logits need their element's alignment
+ * Sums and comparisons are in 64 bits, of exponentials that are right to 1e-10
+ * of themselves: a decision whose two sides are nearer than that may go either
+ * way.  Logits need their element's alignment
  * only (16-byte aligned rows are read faster).  A sequence with malformed
  * offsets, or that reaches a draft out of range or a row that is no
  * distribution (NaN, +infinity or nothing above -infinity), keeps the drafts

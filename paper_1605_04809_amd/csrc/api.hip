@@ -1507,9 +1507,9 @@ nmt_status nmt_step_readouts(nmt_model* m, const nmt_source* src, int32_t B, con
 }
 
 // The vocabulary kernels' passes over the weights with the logits stored: 5 rows
-// of E = 500, V = 100,000 with fp32 weights 40 us (202 MB at the rate of a large
-// copy, 4.9 TB/s), 320 with bf16 ones 72 us (229 MB, 129 of them stores; the
-// kernel 64, the sums' merge 5).
+// of E = 500, V = 100,000 with fp32 weights 40 us (202 MB at 5.0 TB/s, where
+// reading alone goes at 6.3; the kernel 36, the sums' merge 4), 320 with bf16
+// ones 72 to 77 us (229 MB, 128 of them stores; the kernel 64, the merge 5).
 nmt_status nmt_logits(nmt_model* m, int32_t M, const float* d_t, float* d_logits, int64_t ld_logits, float* d_logZ,
                       void* d_workspace, size_t ws_bytes, void* stream) {
   if (!m) return fail(NMT_EINVAL, "NULL model");

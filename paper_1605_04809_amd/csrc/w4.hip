@@ -214,7 +214,7 @@ struct W4Shape {
 };
 // Waves a block, and K blocks in flight.  Many rows, or a K that is long for 16
 // rows, fill a CU's LDS by themselves, so their block is 16 waves (80 rows of K
-// = 500, N = 100,000: 51 us with 8, 32 with 16); the others leave room for two
+// = 500, N = 100,000: 30 us, and 1.6 times that with 8); the others leave room for two
 // blocks, and a wave for the whole K of an output layer (33 rows of 1001 x
 // 7777: 10.1 us with two K blocks in flight, 9.1 with four).
 constexpr int w4_waves(int RM, bool long_k) { return RM > 16 || (RM == 16 && long_k) ? 16 : 8; }
