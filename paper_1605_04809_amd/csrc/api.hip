@@ -988,10 +988,14 @@ nmt_status nmt_model_create(const nmt_dims* dims, const nmt_weights* w, nmt_mode
       if (!bf16) {
         brows[(size_t)v] = b;
       } else {
-        const float hi = bf16_value(b), mid = bf16_value(b - hi);
+        // (one that masks its word stays whole: an infinity is all in hi, and a
+        // finite bias next to fp32's largest values does not round up to one)
+        float hi = bf16_value(b);
+        if (std::isinf(hi) && !std::isinf(b)) hi = std::copysign(0x1.fep127f, b);
+        const float left = std::isinf(b) ? 0.f : b - hi, mid = bf16_value(left);
         brows[(size_t)v] = hi;
         brows[(size_t)V + v] = mid;
-        brows[(size_t)2 * V + v] = b - hi - mid;  // exact in bf16: what remains has at most 8 significant bits
+        brows[(size_t)2 * V + v] = left - mid;  // exact in bf16: what remains has at most 8 significant bits
       }
     }
     Seg sg{w->out_W, E, V, brows.data(), nb};

@@ -425,3 +425,41 @@ def test_logits_of_small_rows(wtype, spoil):
     print(wtype, spoil, worst, flush=True)
     assert np.all(worst <= 1.0)
     model.close()
+
+
+@pytest.mark.parametrize("wtype", ["f32", "bf16"])
+def test_words_that_the_bias_masks(wtype):
+    """Biases of -infinity or fp32's lowest value forbid their words, in the logits, in the step's log p and in a
+    4-bit copy of the layer; the other words' are as they are without such words."""
+    torch = _torch()
+    from paper_1605_04809_amd import binding as nb
+    wl = make_workload(CONFIGS["tiny"].replace(seed=36, sigma_w=0.2, wtype=wtype))
+    c, low = wl.cfg, np.finfo(np.float32).min
+    masked = {3: -np.inf, c.V - 1: -np.inf, 70: low, 500: low}
+    for v, b in masked.items():
+        wl.params["out_b"][v] = b
+    run = GpuRun(wl)
+    req = wl.req.copy()
+    req[:4] = list(masked)
+    step = run.step(wl.s_prev, wl.y_prev, wl.sent_id, req)
+    W, b = wl.params["out_W"], wl.params["out_b"].astype(np.float64)
+    W = (dc.round_bf16(W) if wtype == "bf16" else W).astype(np.float64)
+    t = step["t"]
+    want = t.astype(np.float64) @ W + b
+    z, lz = _logits(torch, nb, run.model, t)
+    rest = np.setdiff1d(np.arange(c.V), list(masked))
+    assert np.isneginf(z[:, [3, c.V - 1]]).all() and (z[:, [70, 500]] < -3.4e38).all()
+    _check_logits(z[:, rest], None, t, W[:, rest], b[rest])
+    wlz = np.log(np.exp(want[:, rest]).sum(1))
+    tol = 2.0 ** -24 * ((c.E + 16) * (np.abs(t) @ np.abs(W[:, rest]) + np.abs(b[rest])).max(1) + c.V / 256 + 256)
+    for got in (lz, step["logZ"]):
+        assert np.all(np.abs(got - wlz) <= tol + 2.0 ** -23 * np.abs(wlz))
+    assert np.isneginf(step["logp"][:2]).all() and (step["logp"][2:4] < -3.4e38).all()
+    assert np.isfinite(step["logp"][4:]).all()
+    w4 = nb.W4.from_output(run.model, 32)
+    y = torch.zeros((c.B, c.V), device="cuda")
+    nb.nmt_w4_product(w4, cuda(t), y)
+    y = y.cpu().numpy()
+    assert np.isneginf(y[:, [3, c.V - 1]]).all() and (y[:, [70, 500]] < -3.4e38).all() and np.isfinite(y[:, rest]).all()
+    w4.close()
+    run.close()
